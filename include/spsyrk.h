@@ -47,7 +47,8 @@ typedef enum {
     SPSYRK_ERR_NOT_IMPLEMENTED = 8
 } spsyrk_status_t;
 
-typedef enum { SPSYRK_F64 = 0, SPSYRK_F32 = 1, SPSYRK_I32 = 2 } spsyrk_dtype_t;
+/* SPSYRK_BF16 and SPSYRK_F16 are taken by spsyrk_lookup and what follows it only. */
+typedef enum { SPSYRK_F64 = 0, SPSYRK_F32 = 1, SPSYRK_I32 = 2, SPSYRK_BF16 = 3, SPSYRK_F16 = 4 } spsyrk_dtype_t;
 
 /* SPSYRK_TRIL keeps products a_ik * a_jk with j <= i only (Section III-A: a diagonal process
  * computes only the lower triangle; Algorithm 2, line 2).  SPSYRK_FULL removes the cut-off and
@@ -381,6 +382,93 @@ spsyrk_status_t spsyrk_jaccard(int64_t m, int64_t row_begin, int64_t rows,
  * caller-owned and must be valid during every later spsyrk_numeric call.  Errors: INVALID_ARG.
  */
 spsyrk_status_t spsyrk_plan_set_jaccard(spsyrk_plan_t plan, float *d_jaccard);
+
+/*
+ * Products of CSR rows of ids with dense matrices: the two ends of a model over a vocabulary of n ids.
+ *
+ * A is an m x n matrix whose row i holds the entries [d_rowptr[i], d_rowptr[i + 1]) of d_ids and d_weights, or, with
+ * d_rowptr == NULL, the nnz / m entries that follow those of the row before (nnz a multiple of m; nnz == m: one id a row, an
+ * ordinary table lookup).  Unlike the matrices above it need not be canonical: ids may come in any order and as often as they
+ * like, and an id outside [0, n) stands for padding: it contributes nothing and receives nothing.  Entries before d_rowptr[0] and
+ * behind d_rowptr[m] belong to no row.  Row pointers must ascend; if they do not, or point outside [0, nnz], the result is unspecified,
+ * but nothing outside the arrays is touched.
+ * Dense matrices are row-major with a row stride in elements (ld* >= the row's length) of SPSYRK_F64, F32, BF16 or F16; what lies
+ * between the rows is neither read nor written.  16-byte aligned rows are read fastest.  Sums are held in double for
+ * F64 and in single precision otherwise, in an order that depends on sizes and alignment only, and rounded once: the same call gives the
+ * same bits.  All of these calls are asynchronous and can be captured into a graph.
+ * Common errors: INVALID_ARG (a null pointer with something to read or write behind it, a negative size, a stride below the row's
+ * length, nnz not a multiple of m without row pointers, a type that is not listed), OVERFLOW (m, n or nnz >= 2^31 - 1, p > 2^22), CUDA.
+ */
+
+/*
+ * spsyrk_lookup - Y = scale * A E:   y[i, :] = scale * sum over the entries t of row i of  w_t * E[id_t, :].
+ * E is n x p and Y m x p, both of `dtype`; d_weights has nnz values (double for F64, else float), NULL: all one.  A row without
+ * entries gives zeros.  Y must not alias E.
+ */
+spsyrk_status_t spsyrk_lookup(int64_t m, int64_t n, int64_t p, int64_t nnz, spsyrk_dtype_t dtype,
+                              const int64_t *d_rowptr, const int32_t *d_ids, const void *d_weights, double scale,
+                              const void *d_e, int64_t lde, void *d_y, int64_t ldy, void *cuda_stream);
+
+/*
+ * spsyrk_lookup_grad - the gradient of spsyrk_lookup with respect to the table, dE = scale * A^T dY:
+ *     dE[v, :] = scale * sum over the entries t with id v of  w_t * dY[row of t, :],
+ * by a stable sort of the ids; the entries of an id are added up in pieces of a fixed length, the pieces in their order.
+ * dY is m x p of `dtype`; dE is n x p of `g_dtype`, which is `dtype` or, for half precision, SPSYRK_F32 (a gradient that is kept
+ * in single precision).  accumulate == 0: dE is overwritten, zeros in the rows of ids that do not occur.
+ * accumulate != 0: dE += the gradient, one more addition before the rounding; the rows of ids that do not occur are not touched.
+ *
+ * Two-step use: d_workspace == NULL: *workspace_bytes receives the scratch size for (m, n, p, nnz, dtype) with and without row pointers
+ * and weights; then the call, with a workspace of at least that size, 256-byte aligned, that no other work uses until this has ended.
+ * Errors also: WORKSPACE.
+ */
+spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t g_dtype,
+                                   const int64_t *d_rowptr, const int32_t *d_ids, const void *d_weights, double scale,
+                                   const void *d_dy, int64_t lddy, void *d_de, int64_t ldde, int accumulate,
+                                   void *d_workspace, size_t *workspace_bytes, void *cuda_stream);
+
+/*
+ * spsyrk_lookup_grad_weights - the gradient of spsyrk_lookup with respect to the weights:
+ *     dw_t = scale * <E[id_t, :], dY[row of t, :]>   (0 for padding and for entries of no row),   nnz values, double for F64,
+ * else float.
+ */
+spsyrk_status_t spsyrk_lookup_grad_weights(int64_t m, int64_t n, int64_t p, int64_t nnz, spsyrk_dtype_t dtype,
+                                           const int64_t *d_rowptr, const int32_t *d_ids, double scale,
+                                           const void *d_e, int64_t lde, const void *d_dy, int64_t lddy, void *d_dw,
+                                           void *cuda_stream);
+
+/*
+ * spsyrk_distill - distillation from a teacher's top logits.  Row i of the student's logits s (m x n of `dtype`: F32, BF16 or F16)
+ * meets row i of A, whose entries are ids and the teacher's logits z (d_teacher, nnz values of `teacher_dtype`: F32, BF16 or F16).
+ * With the temperature tau (1e-6 to 1e6; INVALID_ARG beyond):
+ *     p_t    = exp(z_t / tau - L_i),     L_i = log sum over the entries of exp(z_t / tau), or d_teacher_lse[i] (float) if it is given:
+ *                                        the logarithm of the sum over the teacher's whole vocabulary
+ *     q_v    = exp(s_iv / tau - lse_i),  lse_i = log sum over the n ids of exp(s_iv / tau)
+ *     loss_i = scale * r_i * sum over the entries of  p_t * (log p_t - log q_{id_t})            (r = d_row_weights, NULL: one)
+ *     G_iv   = scale * r_i / tau * (P_i * q_v - sum over the entries with id v of p_t),   P_i = sum over the entries of p_t,
+ * the gradient of the sum of all losses.  (scale = tau^2 keeps gradients alike over temperatures.)  Entries whose p_t is 0 add nothing.
+ * A row is left out if its weight is 0 or none of its entries is an id in [0, n) with a logit other than -infinity: its loss and
+ * lse are 0, its gradient is 0, its logits are not looked at.  NaN or +infinity among the logits that a row is computed from, the student's
+ * or the teacher's, make its loss and its whole gradient NaN, and so do a student's logits that are all -infinity.
+ * d_loss[m] and d_lse[m] are float and may be NULL; G is m x n of `dtype`, NULL: no gradient, else computed in the same pass.
+ * G may be s itself (same stride), else it must not alias s.
+ */
+spsyrk_status_t spsyrk_distill(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t teacher_dtype,
+                               const int64_t *d_rowptr, const int32_t *d_ids, const void *d_teacher, const float *d_teacher_lse,
+                               const float *d_row_weights, double temperature, double scale,
+                               const void *d_logits, int64_t ldl, float *d_loss, float *d_lse, void *d_grad, int64_t ldg,
+                               void *cuda_stream);
+
+/*
+ * spsyrk_distill_grad - G of spsyrk_distill from the lse that a call without G has returned: the backward pass when the rows'
+ * weights (the gradient of the losses times the weights of the forward pass) come later.  A row that was left out there must be
+ * left out here.  (Logits that are all beyond 1e30 in size, as in a row that is masked throughout with the type's lowest value, leave no
+ * room in lse for the rest of the sum: such a row's gradient is NaN here.)  Other arguments as there.
+ */
+spsyrk_status_t spsyrk_distill_grad(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t teacher_dtype,
+                                    const int64_t *d_rowptr, const int32_t *d_ids, const void *d_teacher, const float *d_teacher_lse,
+                                    const float *d_row_weights, double temperature, double scale,
+                                    const void *d_logits, int64_t ldl, const float *d_lse, void *d_grad, int64_t ldg,
+                                    void *cuda_stream);
 
 /*
  * spsyrk_plan_stats - host-side facts about a plan.

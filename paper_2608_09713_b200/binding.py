@@ -24,12 +24,13 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 OK = 0
-F64, F32, I32 = 0, 1, 2
+F64, F32, I32, BF16, F16 = 0, 1, 2, 3, 4
 TRIL, FULL = 0, 1
 NCLASS = 8
 
 _DTYPE_CODE = {torch.float64: F64, torch.float32: F32, torch.int32: I32}
 _CODE_DTYPE = {v: k for k, v in _DTYPE_CODE.items()}
+_REAL_CODE = {torch.float64: F64, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}  # dense matrices of spsyrk_lookup and what follows it
 
 _i64, _vp, _int = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int
 _szp = ctypes.POINTER(ctypes.c_size_t)
@@ -69,6 +70,17 @@ _lib.spsyrk_symv.argtypes = [_i64, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.spsyrk_symv.restype = _int
 _lib.spsyrk_symm.argtypes = [_i64, _i64, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.spsyrk_symm.restype = _int
+_f64 = ctypes.c_double
+_lib.spsyrk_lookup.argtypes = [_i64, _i64, _i64, _i64, _int, _vp, _vp, _vp, _f64, _vp, _i64, _vp, _i64, _vp]
+_lib.spsyrk_lookup.restype = _int
+_lib.spsyrk_lookup_grad.argtypes = [_i64, _i64, _i64, _i64, _int, _int, _vp, _vp, _vp, _f64, _vp, _i64, _vp, _i64, _int, _vp, _szp, _vp]
+_lib.spsyrk_lookup_grad.restype = _int
+_lib.spsyrk_lookup_grad_weights.argtypes = [_i64, _i64, _i64, _i64, _int, _vp, _vp, _f64, _vp, _i64, _vp, _i64, _vp, _vp]
+_lib.spsyrk_lookup_grad_weights.restype = _int
+_lib.spsyrk_distill.argtypes = [_i64, _i64, _i64, _int, _int, _vp, _vp, _vp, _vp, _vp, _f64, _f64, _vp, _i64, _vp, _vp, _vp, _i64, _vp]
+_lib.spsyrk_distill.restype = _int
+_lib.spsyrk_distill_grad.argtypes = [_i64, _i64, _i64, _int, _int, _vp, _vp, _vp, _vp, _vp, _f64, _f64, _vp, _i64, _vp, _vp, _i64, _vp]
+_lib.spsyrk_distill_grad.restype = _int
 _lib.spsyrk_jaccard.argtypes = [_i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.spsyrk_plan_stats.argtypes = [_vp, _i64p, _i64p]
 _lib.spsyrk_plan_buffers.argtypes = [_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp), ctypes.POINTER(_vp), ctypes.POINTER(_vp)]
@@ -518,6 +530,194 @@ def spsyrk_jaccard(m, row_begin, rows, a_rowptr, c_rowptr, c_colidx, c_counts, o
     _check(_lib.spsyrk_jaccard(m, row_begin, rows, _p(a_rowptr), _p(c_rowptr), _p(c_colidx), _p(c_counts), _p(out),
                                _stream(stream)), "spsyrk_jaccard")
     return out
+
+
+# ------------------------------------------------------------------------------------------
+# Rows of ids and dense matrices: lookups, their gradients, distillation.  The work goes to the tensors' device whatever the
+# current one is, to `stream` or to the current stream of that device.
+# ------------------------------------------------------------------------------------------
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(fn, where, tensors, stream, *args):
+    """fn(*args, stream) on the device of the tensors (None among them is skipped), which must be one."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise ValueError(f"{where}: tensors must be CUDA tensors on one device")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{where}: the stream belongs to another device")
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if device.index == torch.cuda.current_device():
+        status = fn(*args, s.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, s.cuda_stream)
+    if status != OK:
+        raise SpsyrkError(status, where)
+
+
+def _matrix(t, where, name, rows=None, cols=None, dtype=None):
+    """The row stride of a dense matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in _REAL_CODE or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{where}: {name} must be a matrix of {dtype or 'float64, float32, bfloat16 or float16'}")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not ({rows}, {cols})")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{where}: the rows of {name} must be contiguous")
+    if t.shape[0] < 2:
+        return max(t.shape[1], 1)
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(f"{where}: the rows of {name} overlap")
+    return t.stride(0)
+
+
+def _entries(where, ids, rowptr, values, dtypes, name):
+    """Rows and entries of a matrix given by ids and row pointers, or by ids with as many entries in every row."""
+    if ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError(f"{where}: ids must be contiguous int32")
+    if rowptr is None:
+        if ids.dim() not in (1, 2):
+            raise ValueError(f"{where}: ids without row pointers have one or two dimensions")
+        m = ids.shape[0]
+    else:
+        if rowptr.dtype != torch.int64 or rowptr.dim() != 1 or rowptr.numel() < 1 or not rowptr.is_contiguous() or ids.dim() != 1:
+            raise ValueError(f"{where}: row pointers must be contiguous int64, at least one, and ids then have one dimension")
+        m = rowptr.numel() - 1
+    if values is not None and (values.dtype not in dtypes or values.shape != ids.shape or not values.is_contiguous()):
+        raise ValueError(f"{where}: {name} must be contiguous, {' or '.join(map(str, dtypes))}, one for each id")
+    return m, ids.numel()
+
+
+def _weight_dtype(dtype):
+    return torch.float64 if dtype == torch.float64 else torch.float32
+
+
+def spsyrk_lookup(ids, e, rowptr=None, weights=None, scale=1.0, y=None, stream=None):
+    """Y = scale * A E, shape (m, p): ids of shape (m,), one a row, or (m, k), or (nnz,) with row pointers; weights as the ids
+    (float64 for a float64 table, else float32) or None; e the table, (n, p).  An id outside [0, n) is padding."""
+    lde = _matrix(e, "spsyrk_lookup", "e")
+    m, nnz = _entries("spsyrk_lookup", ids, rowptr, weights, (_weight_dtype(e.dtype),), "weights")
+    n, p = e.shape
+    if y is None:
+        y = torch.empty((m, p), dtype=e.dtype, device=e.device)
+        ldy = max(p, 1)
+        _in_use_on(stream, y)
+    else:
+        ldy = _matrix(y, "spsyrk_lookup", "y", m, p, e.dtype)
+    _call(_lib.spsyrk_lookup, "spsyrk_lookup", (ids, e, rowptr, weights, y), stream, m, n, p, nnz, _REAL_CODE[e.dtype], _ptr(rowptr), ids.data_ptr(),
+          _ptr(weights), scale, e.data_ptr(), lde, y.data_ptr(), ldy)
+    return y
+
+
+def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None, accumulate=False, dtype=None, workspace=None, stream=None):
+    """dE = scale * A^T dY, shape (n, p), of `dtype` (that of dy, or float32 for half precision); `de` is overwritten, or
+    added to when `accumulate`.  `workspace`: a uint8 CUDA tensor that no other work uses until this has ended."""
+    where = "spsyrk_lookup_grad"
+    m, nnz = _entries(where, ids, rowptr, weights, (_weight_dtype(dy.dtype),), "weights")
+    lddy = _matrix(dy, where, "dy", m)
+    p = dy.shape[1]
+    if de is None:
+        if accumulate:
+            raise ValueError(f"{where}: nothing to add to")
+        dtype = dy.dtype if dtype is None else dtype
+        if dtype not in _REAL_CODE:
+            raise ValueError(f"{where}: no gradients of {dtype}")
+        de = torch.empty((n, p), dtype=dtype, device=dy.device)
+        ldde = max(p, 1)
+        _in_use_on(stream, de)
+    else:
+        ldde = _matrix(de, where, "de", n, p, dtype)
+    sz = ctypes.c_size_t(0)
+    code, g_code = _REAL_CODE[dy.dtype], _REAL_CODE[de.dtype]
+    _check(_lib.spsyrk_lookup_grad(m, n, p, nnz, code, g_code, None, None, None, scale, None, lddy, None, ldde, 0, None, ctypes.byref(sz), None),
+           f"{where}(size query)")
+    if workspace is None:
+        workspace = _workspace(sz.value, dy.device)
+        _in_use_on(stream, workspace)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError(f"{where}: the workspace must be contiguous uint8")
+    sz.value = workspace.numel()
+    _call(_lib.spsyrk_lookup_grad, where, (ids, dy, rowptr, weights, de, workspace), stream, m, n, p, nnz, code, g_code, _ptr(rowptr), ids.data_ptr(),
+          _ptr(weights), scale, dy.data_ptr(), lddy, de.data_ptr(), ldde, 1 if accumulate else 0, workspace.data_ptr(), ctypes.byref(sz))
+    return de
+
+
+def spsyrk_lookup_grad_weights(ids, e, dy, rowptr=None, scale=1.0, dw=None, stream=None):
+    """dw_t = scale * <E[id_t], dY[row of t]>, shaped as the ids: the gradient of the weights."""
+    where = "spsyrk_lookup_grad_weights"
+    lde = _matrix(e, where, "e")
+    if dw is None:
+        dw = torch.empty(ids.shape, dtype=_weight_dtype(e.dtype), device=e.device)
+        _in_use_on(stream, dw)
+    m, nnz = _entries(where, ids, rowptr, dw, (_weight_dtype(e.dtype),), "dw")
+    n, p = e.shape
+    lddy = _matrix(dy, where, "dy", m, p, e.dtype)
+    _call(_lib.spsyrk_lookup_grad_weights, where, (ids, e, dy, rowptr, dw), stream, m, n, p, nnz, _REAL_CODE[e.dtype], _ptr(rowptr), ids.data_ptr(), scale,
+          e.data_ptr(), lde, dy.data_ptr(), lddy, dw.data_ptr())
+    return dw
+
+
+_LOGITS = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights):
+    ldl = _matrix(logits, where, "logits")
+    if logits.dtype not in _LOGITS:
+        raise ValueError(f"{where}: logits must be float32, bfloat16 or float16")
+    m, nnz = _entries(where, ids, rowptr, teacher, _LOGITS, "the teacher's logits")
+    if logits.shape[0] != m:
+        raise ValueError(f"{where}: {m} rows of the teacher and {logits.shape[0]} of the student")
+    for t in (teacher_lse, row_weights):
+        if t is not None and (t.dtype != torch.float32 or t.shape != (m,) or not t.is_contiguous()):
+            raise ValueError(f"{where}: teacher_lse and row_weights must be contiguous float32, one for each row")
+    return m, nnz, ldl
+
+
+def _gradient(where, logits, ldl, grad, stream):
+    """The gradient's matrix and row stride; the rows of a new one lie to 16-byte boundaries as those of the logits do."""
+    if grad is None or grad is True:
+        m, n = logits.shape
+        ldg = max(n + (ldl - n) % (16 // logits.element_size()), 1)
+        grad = torch.empty((m, ldg), dtype=logits.dtype, device=logits.device)[:, :n]
+        _in_use_on(stream, grad)
+        return grad, ldg
+    return grad, _matrix(grad, where, "grad", *logits.shape, logits.dtype)
+
+
+def spsyrk_distill(logits, ids, teacher, rowptr=None, teacher_lse=None, row_weights=None, temperature=1.0, scale=None, grad=None, stream=None):
+    """Distillation from a teacher's top logits: (loss, lse) of every row, float32.  The teacher's ids and logits have shape (m, k), or
+    (nnz,) with row pointers.  With `grad` (True, or a matrix; `logits` itself is allowed) also the gradient of the sum of all losses,
+    as a third result.  `scale` is temperature^2 unless it is given."""
+    where = "spsyrk_distill"
+    m, nnz, ldl = _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights)
+    both = torch.empty((2, m), dtype=torch.float32, device=logits.device)
+    _in_use_on(stream, both)
+    loss, lse = both.unbind(0)
+    with_grad, ldg = grad is not None and grad is not False, 0
+    if with_grad:
+        grad, ldg = _gradient(where, logits, ldl, grad, stream)
+    else:
+        grad = None
+    _call(_lib.spsyrk_distill, where, (logits, ids, teacher, rowptr, teacher_lse, row_weights, grad), stream, m, logits.shape[1], nnz, _REAL_CODE[logits.dtype],
+          _REAL_CODE[teacher.dtype], _ptr(rowptr), ids.data_ptr(), teacher.data_ptr(), _ptr(teacher_lse), _ptr(row_weights), temperature,
+          temperature * temperature if scale is None else scale, logits.data_ptr(), ldl, loss.data_ptr(), lse.data_ptr(), _ptr(grad), ldg)
+    return (loss, lse, grad) if with_grad else (loss, lse)
+
+
+def spsyrk_distill_grad(logits, lse, ids, teacher, rowptr=None, teacher_lse=None, row_weights=None, temperature=1.0, scale=None, grad=None, stream=None):
+    """The gradient that spsyrk_distill gives, from the lse that it returned: for rows' weights that are known later only.  `grad`: a
+    matrix (`logits` itself is allowed) or None for a new one."""
+    where = "spsyrk_distill_grad"
+    m, nnz, ldl = _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights)
+    if lse.dtype != torch.float32 or lse.shape != (m,) or not lse.is_contiguous():
+        raise ValueError(f"{where}: lse must be contiguous float32, one for each row")
+    grad, ldg = _gradient(where, logits, ldl, grad, stream)
+    _call(_lib.spsyrk_distill_grad, where, (logits, lse, ids, teacher, rowptr, teacher_lse, row_weights, grad), stream, m, logits.shape[1], nnz,
+          _REAL_CODE[logits.dtype], _REAL_CODE[teacher.dtype], _ptr(rowptr), ids.data_ptr(), teacher.data_ptr(), _ptr(teacher_lse), _ptr(row_weights),
+          temperature, temperature * temperature if scale is None else scale, logits.data_ptr(), ldl, lse.data_ptr(), grad.data_ptr(), ldg)
+    return grad
 
 
 def spsyrk_host_tril(m, n, rowptr, colidx, vals, mode=TRIL, pinned=True, out=None):

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspsyrk.so")
 LIB_CHECKED = os.path.join(HERE, "libspsyrk_checked.so")  # same sources with -DSPSYRK_CHECKED (bounds-checked indices)
-SOURCES = ["api.cu", "mirror.cu", "jaccard.cu", "symv.cu", "accumulate.cu", "permute.cu", "host.cu"]
+SOURCES = ["api.cu", "mirror.cu", "jaccard.cu", "symv.cu", "accumulate.cu", "permute.cu", "host.cu", "lookup.cu",
+           "lookup_grad.cu", "distill.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
               "-Wno-deprecated-gpu-targets"]

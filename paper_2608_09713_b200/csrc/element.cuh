@@ -1,0 +1,127 @@
+// What the products of CSR rows of ids with dense row-major matrices share: element types, vectors of elements, rows of entries.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace spsyrk {
+
+// The type sums are held in: double for double, else single precision.
+template <typename T> struct Wide { using type = float; };
+template <> struct Wide<double> { using type = double; };
+
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ double widen(double v) { return v; }
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float widen(__half v) { return __half2float(v); }
+
+// One rounding, to nearest even.
+template <typename T, typename A> __device__ __forceinline__ T narrow(A v);
+template <> __device__ __forceinline__ float narrow<float, float>(float v) { return v; }
+template <> __device__ __forceinline__ double narrow<double, double>(double v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16, float>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half narrow<__half, float>(float v) { return __float2half_rn(v); }
+
+// W elements that are read and written together, 16 bytes at most; their address is a multiple of their size.
+template <typename T, int W>
+struct alignas(sizeof(T) * W) Vec {
+    static_assert(sizeof(T) * W <= 16, "16 bytes");
+    T x[W];
+};
+template <typename T, int V> constexpr int VEC_OF = V * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : V;
+
+// the first `left` elements at p, widened, zeros behind them
+template <typename T, int V>
+__device__ __forceinline__ void load_wide(const T* __restrict__ p, int64_t left, typename Wide<T>::type (&x)[V]) {
+    constexpr int W = VEC_OF<T, V>;
+    if (left >= V) {
+#pragma unroll
+        for (int k = 0; k < V; k += W) {
+            const Vec<T, W> v = *reinterpret_cast<const Vec<T, W>*>(p + k);
+#pragma unroll
+            for (int i = 0; i < W; ++i) x[k + i] = widen(v.x[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = i < left ? widen(p[i]) : typename Wide<T>::type(0);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_narrow(T* __restrict__ p, int64_t left, const typename Wide<T>::type (&x)[V]) {
+    constexpr int W = VEC_OF<T, V>;
+    if (left >= V) {
+#pragma unroll
+        for (int k = 0; k < V; k += W) {
+            Vec<T, W> v;
+#pragma unroll
+            for (int i = 0; i < W; ++i) v.x[i] = narrow<T>(x[k + i]);
+            *reinterpret_cast<Vec<T, W>*>(p + k) = v;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < left) p[i] = narrow<T>(x[i]);
+    }
+}
+
+inline size_t element_size(spsyrk_dtype_t t) { return t == SPSYRK_F64 ? 8 : t == SPSYRK_BF16 || t == SPSYRK_F16 ? 2 : 4; }
+inline bool is_real(spsyrk_dtype_t t) { return t == SPSYRK_F64 || t == SPSYRK_F32 || t == SPSYRK_BF16 || t == SPSYRK_F16; }
+inline bool aligned16(const void* p, int64_t ld, size_t size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)size % 16 == 0; }
+
+// Rows of entries: row pointers, or the same number of entries k in every row.  Row pointers are cut to [0, nnz], so that no
+// entry is looked for outside the arrays whatever they hold.
+struct Rows {
+    const int64_t* rowptr;
+    int64_t m, nnz, k;
+    __device__ __forceinline__ int64_t begin(int64_t i) const { return rowptr ? max((int64_t)0, min(rowptr[i], nnz)) : i * k; }
+    __device__ __forceinline__ int64_t end(int64_t i) const { return rowptr ? max((int64_t)0, min(rowptr[i + 1], nnz)) : (i + 1) * k; }
+    // entries before the first row and behind the last one belong to none
+    __device__ __forceinline__ bool covered(int64_t e) const { return !rowptr || (e >= rowptr[0] && e < rowptr[m]); }
+    // the last row in [lo, hi] that begins at entry e or before
+    __device__ __forceinline__ int64_t row_of(int64_t e, int64_t lo, int64_t hi) const {
+        if (!rowptr) return e / k;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) >> 1;
+            if (rowptr[mid] <= e) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    }
+};
+
+// Thread-block clusters: this CTA's number, the number of CTAs, a barrier, and values in another CTA's shared memory.
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive;\nbarrier.cluster.wait;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t address_in(const void* mine, uint32_t rank) {
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    return there;
+}
+__device__ __forceinline__ float load_of_rank(const float* mine, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(address_in(mine, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ double load_of_rank(const double* mine, uint32_t rank) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(address_in(mine, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 load_of_rank(const float2* mine, uint32_t rank) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(address_in(mine, rank)) : "memory");
+    return v;
+}
+
+}  // namespace spsyrk
