@@ -1,15 +1,18 @@
 // Distillation from a teacher's top logits: rows of ids and teacher's logits z (CSR) meet dense rows of a student's logits s.
 // With x = s / tau, lse = log sum_v exp(x_v), q_v = exp(x_v - lse), p_t = exp(z_t / tau - L):
-//     loss = scale r (sum_t p_t (z_t - s_t) / tau + P (lse - L)),      G_v = scale r / tau (P q_v - sum of the p_t with id v).
+//     loss = scale r sum_t p_t (log p_t - log q_{id_t}),      G_v = scale r / tau (P q_v - sum of the p_t with id v).
 //
-// Bound by memory: the logits are read once (running maximum and sum, no second pass for the maximum), and the gradient written once; when
-// both are asked for, the row is read again for the gradient as soon as its sum is known, while it still lies in L2 (a row is
-// 16 KB to 1 MB, those in flight together are far below 126 MB).  A cluster of 1 to 8 CTAs takes a row, so that few rows still use
-// many SMs.  exp(x) is computed as 2^(s * log2(e) / tau - ...), one multiply-add and one exponential per logit.
+// Bound by memory: the logits are read once and the gradient is written once.  A cluster of 1 to 8 CTAs takes a row, each a contiguous
+// share of it, which is copied to shared memory (cp.async, every thread the 16-byte units that it will use itself, so that nobody waits
+// for anybody) while the teacher's entries are looked at; a running maximum and sum per thread, joined over the CTA and the cluster; then the
+// gradient from the copies.  (Reading the row a second time instead finds it in L2 only in part: 296 rows of 256 KB and their gradients
+// are more than L2 holds; 605 us for 4096 rows of 131072 bfloat16 logits, 160 us for a quarter of them at an L2 hit rate of 9 %.)
+// A share that shared memory does not hold goes through it in rounds.
+// exp(x) is computed as 2^(s * log2(e) / tau - ...): a multiply-add (two logits per instruction) and an exponential per logit.
 // The gradient is first written for all ids as if they were not the teacher's, then the few of the teacher's are overwritten, from
-// logits that were fetched beforehand (so the gradient may overwrite the logits).  An id that occurs more than once is
-// written by its first entry, with the sum of its entries in their order: they are found with a hash table in shared memory.  Rows of
-// more than TOP entries go through the ids in windows instead.
+// logits that were fetched beforehand (so the gradient may overwrite the logits).  An id that occurs more than once is written for one
+// of its entries, with the sum of all in their order: they are found with a hash table in shared memory.  Rows of more than
+// 1024 entries (ragged rows: of four times the mean) go through the ids in windows instead.
 #include <algorithm>
 #include <math_constants.h>
 
@@ -19,10 +22,21 @@ using namespace spsyrk;
 
 namespace {
 
-constexpr int THREADS = 512;
+#ifndef DISTILL_THREADS
+#define DISTILL_THREADS 256
+#endif
+#ifndef DISTILL_WARPS_PER_SM
+#define DISTILL_WARPS_PER_SM 24
+#endif
+#ifndef DISTILL_SHARE
+#define DISTILL_SHARE 65536
+#endif
+constexpr int THREADS = DISTILL_THREADS;
 constexpr int WARPS = THREADS / 32;
-constexpr int TOP = 1024;         // teacher's entries of a row that are kept in shared memory
-constexpr int TABLE = 2 * TOP;    // slots of the hash table; of a window's ids in rows of more entries
+constexpr int MOST_TOP = 1024;    // teacher's entries of a row that are kept in shared memory, at most
+constexpr int LEAST_TOP = 32;
+constexpr int WINDOW = 2048;      // ids of a window in rows of more entries
+constexpr int FEWEST_UNITS = WINDOW * 4 / 16;  // 16-byte units of the copy: the windows' table takes its place
 constexpr int SMS = 148;
 constexpr int NONE = 0x7fffffff;
 constexpr double LOG2E = 1.4426950408889634, LN2 = 0.6931471805599453;
@@ -58,6 +72,9 @@ __device__ __forceinline__ float step_down(float from, float to, float k) {  // 
     if (fabsf(to) < LARGE && fabsf(from) < LARGE) return power_of_two(__fmul_rn(from, k) - __fmul_rn(to, k));
     return power_of_two((from - to) * k);
 }
+__device__ __forceinline__ float term(float s, float base, float k) {
+    return power_of_two(fabsf(base) < LARGE ? fmaf(s, k, -__fmul_rn(base, k)) : (s - base) * k);
+}
 template <int N>
 __device__ __forceinline__ void take(Running& r, const float (&s)[N], float k) {
     float top = s[0];
@@ -67,48 +84,180 @@ __device__ __forceinline__ void take(Running& r, const float (&s)[N], float k) {
         r.sum *= step_down(r.most, top, k);  // most = -infinity: times 0
         r.most = top;
     }
+    const float b = base_of(r.most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.sum += term(s[i], b, k);
+}
+// Running sums of N lanes (a power of two, the same ones in all groups of N) joined; all lanes get the same bits.
+template <int N>
+__device__ __forceinline__ Running join(Running r, float k) {
+    float top;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(r.most));
+    r.sum *= step_down(r.most, base_of(top), k);  // (0 times 0 for a lane that has nothing; NaN stays NaN)
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) r.sum += __shfl_xor_sync(FULL_MASK, r.sum, o);
+    return Running{top, r.sum};
+}
+
+// Two single-precision numbers in one register pair, for the instructions that take two at a time.
+struct Pair {
+    uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ float2 halves(Pair p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+    return f;
+}
+__device__ __forceinline__ Pair multiply_add(Pair a, Pair b, Pair c) {
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return d;
+}
+__device__ __forceinline__ Pair add(Pair a, Pair b) {
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+__device__ __forceinline__ Pair multiply(Pair a, Pair b) {
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
+    return d;
+}
+
+// 16 bytes of logits as pairs, their largest value, and back
+template <typename T> struct Unit;
+template <> struct Unit<float> {
+    static constexpr int PAIRS = 2;
+    static constexpr uint32_t NOTHING = 0xff800000u;  // -infinity
+    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
+        return i == 0 ? pair(__uint_as_float(u.x), __uint_as_float(u.y)) : pair(__uint_as_float(u.z), __uint_as_float(u.w));
+    }
+    template <int U>
+    __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
+        float m = __uint_as_float(u[0].x);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            m = fmaxf(fmaxf(m, __uint_as_float(u[i].x)), __uint_as_float(u[i].y));
+            m = fmaxf(fmaxf(m, __uint_as_float(u[i].z)), __uint_as_float(u[i].w));
+        }
+        return m;
+    }
+    __device__ static __forceinline__ uint4 put(const float2 (&y)[2]) {
+        return uint4{__float_as_uint(y[0].x), __float_as_uint(y[0].y), __float_as_uint(y[1].x), __float_as_uint(y[1].y)};
+    }
+};
+__device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+template <> struct Unit<__nv_bfloat16> {
+    static constexpr int PAIRS = 4;
+    static constexpr uint32_t NOTHING = 0xff80ff80u;
+    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
+        return pair(__uint_as_float(word(u, i) << 16), __uint_as_float(word(u, i) & 0xffff0000u));
+    }
+    template <int U>
+    __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
+        __nv_bfloat162 m = reinterpret_cast<const __nv_bfloat162&>(u[0].x);
+#pragma unroll
+        for (int i = 0; i < 4 * U; ++i) {
+            const uint32_t w = word(u[i / 4], i % 4);
+            m = __hmax2(m, reinterpret_cast<const __nv_bfloat162&>(w));
+        }
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    __device__ static __forceinline__ uint4 put(const float2 (&y)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __float22bfloat162_rn(y[i]);
+            w[i] = reinterpret_cast<const uint32_t&>(b);
+        }
+        return uint4{w[0], w[1], w[2], w[3]};
+    }
+};
+template <> struct Unit<__half> {
+    static constexpr int PAIRS = 4;
+    static constexpr uint32_t NOTHING = 0xfc00fc00u;
+    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
+        const uint32_t w = word(u, i);
+        const float2 f = __half22float2(reinterpret_cast<const __half2&>(w));
+        return pair(f.x, f.y);
+    }
+    template <int U>
+    __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
+        __half2 m = reinterpret_cast<const __half2&>(u[0].x);
+#pragma unroll
+        for (int i = 0; i < 4 * U; ++i) {
+            const uint32_t w = word(u[i / 4], i % 4);
+            m = __hmax2(m, reinterpret_cast<const __half2&>(w));
+        }
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+    __device__ static __forceinline__ uint4 put(const float2 (&y)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 b = __float22half2_rn(y[i]);
+            w[i] = reinterpret_cast<const uint32_t&>(b);
+        }
+        return uint4{w[0], w[1], w[2], w[3]};
+    }
+};
+
+// U units at a time into a running sum
+template <typename T, int U>
+__device__ __forceinline__ void take_units(Running& r, const uint4 (&u)[U], float k) {
+    constexpr int PAIRS = Unit<T>::PAIRS;
+    const float top = Unit<T>::template largest<U>(u);
+    if (top > r.most) {
+        r.sum *= step_down(r.most, top, k);
+        r.most = top;
+    }
     const float b = base_of(r.most), at = __fmul_rn(b, k);
     if (fabsf(b) < LARGE) {
+        const Pair kk = pair(k, k), off = pair(-at, -at);
+        Pair sum[2] = {pair(r.sum, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-        for (int i = 0; i < N; ++i) r.sum += power_of_two(fmaf(s[i], k, -at));
+        for (int i = 0; i < U * PAIRS; ++i) {
+            const float2 x = halves(multiply_add(Unit<T>::get(u[i / PAIRS], i % PAIRS), kk, off));
+            sum[i & 1] = add(sum[i & 1], pair(power_of_two(x.x), power_of_two(x.y)));
+        }
+        const float2 s = halves(add(sum[0], sum[1]));
+        r.sum = s.x + s.y;
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) r.sum += power_of_two((s[i] - b) * k);
+        for (int i = 0; i < U * PAIRS; ++i) {
+            const float2 x = halves(Unit<T>::get(u[i / PAIRS], i % PAIRS));
+            r.sum += power_of_two((x.x - b) * k) + power_of_two((x.y - b) * k);
+        }
     }
 }
-__device__ __forceinline__ Running merge(Running a, Running b, float k) {
-    const float top = fmaxf(a.most, b.most), to = base_of(top);
-    return Running{top, a.sum * step_down(a.most, to, k) + b.sum * step_down(b.most, to, k)};
-}
 
-// Sums and maxima over a CTA; every thread gets the result.  `scratch`: WARPS values that nothing else uses meanwhile.
-template <typename V, typename Op>
-__device__ __forceinline__ V over_cta(V v, V* scratch, Op op) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(FULL_MASK, v, o));
-    __syncthreads();
-    if (lane_id() == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = scratch[0];
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) v = op(v, scratch[w]);
-    return v;
+__device__ __forceinline__ void copy_unit(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
-// The columns [0, n) of a row in this CTA's share: [v0, v1) in units of W elements from the first 16-byte boundary, and, for the
-// first CTA, the `head` elements before it and the elements behind the last unit.
+// A row's columns in 16-byte units from its first 16-byte boundary: this CTA has `units` of them from column `first` on, and the
+// first CTA also the `head` columns before the boundary and those from `tail` on, behind the last unit.
 struct Share {
-    int64_t head, v0, v1, tail;
+    int head, units;
+    int64_t first, tail;
 };
 template <typename T>
-__device__ __forceinline__ Share share_of(const T* row, int64_t n, uint32_t rank, uint32_t size) {
+__device__ __forceinline__ Share share_of(const T* row, int64_t n, uint32_t rank, int log_size) {
     constexpr int W = 16 / (int)sizeof(T);
     Share s;
-    s.head = min(n, (int64_t)((0 - reinterpret_cast<uintptr_t>(row)) % 16 / sizeof(T)));
-    const int64_t units = (n - s.head) / W, each = (units + size - 1) / size;
-    s.v0 = min(units, rank * each);
-    s.v1 = min(units, s.v0 + each);
-    s.tail = s.head + units * W;
+    s.head = (int)min(n, (int64_t)((0 - reinterpret_cast<uintptr_t>(row)) % 16 / sizeof(T)));
+    const int units = (int)((uint32_t)(n - s.head) / W), each = (units + (1 << log_size) - 1) >> log_size, v0 = min(units, (int)rank * each);
+    s.units = min(units - v0, each);
+    s.first = s.head + (int64_t)v0 * W;
+    s.tail = s.head + (int64_t)units * W;
     return s;
 }
 
@@ -122,94 +271,163 @@ struct Call {
     int64_t ldl, ldg;
     float *loss, *lse;
     const float* kept;  // the rows' lse of an earlier call (gradient only)
+    float factor;       // scale / tau
+    int log_cluster;    // CTAs of a row
+    int top, log_slots; // entries that are kept in shared memory; slots of the hash table, at least twice as many
+    int room;           // units that the copy in shared memory holds, a multiple of 2 * THREADS
+};
+
+// What the terms of a running sum are taken relative to, as a logarithm.  (k is rounded, 1 / tau is not: base / tau, and what rounding
+// the product base k moved it by.)
+__device__ __forceinline__ double base_in_nats(float base, const Call& c) {
+    return (double)base * c.inv_tau_d + (fabsf(base) < LARGE ? ((double)__fmul_rn(base, c.k) - (double)base * (double)c.k) * LN2 : 0.0);
+}
+
+// Loss and lse of a row, by a whole CTA; the teacher's entries are in shared memory (`few`) or are read again.
+template <typename T>
+__device__ __forceinline__ void write_loss(const Call& c, int64_t row, float weight, int64_t e0, int64_t entries, bool few, const int32_t* s_id,
+                                           const float* s_z, const float* s_at, const T* s, Running r, float top, Running teacher) {
+    __shared__ double s_sum[WARPS][2];
+    const float b = base_of(r.most);
+    double mass = 0, cross = 0;  // sum of e_t; of e_t tau (log p_t - log q_t), but for the logarithms that all share
+    for (int64_t t = threadIdx.x; t < entries; t += THREADS) {
+        const int32_t id = few ? s_id[t] : c.teacher.ids[e0 + t];
+        if (id < 0 || id >= c.n) continue;
+        const float z = few ? s_z[t] : c.teacher.logit(e0 + t), at = few ? s_at[t] : widen(s[id]);
+        const float e = term(z, top, c.k);
+        if (e == 0.f) continue;
+        mass += (double)e;
+        cross += (double)e * (((double)z - (double)top) - ((double)at - (double)b));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        mass += __shfl_xor_sync(FULL_MASK, mass, o);
+        cross += __shfl_xor_sync(FULL_MASK, cross, o);
+    }
+    if (lane_id() == 0) {
+        s_sum[threadIdx.x >> 5][0] = mass;
+        s_sum[threadIdx.x >> 5][1] = cross;
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < WARPS; ++w) {
+        mass += s_sum[w][0];
+        cross += s_sum[w][1];
+    }
+    // log p = (z - top) / tau + log_unit - slip, log q = (s - b) / tau - rest; p = e * unit
+    const double slip_of_top = base_in_nats(top, c) - (double)top * c.inv_tau_d;
+    const double rest = base_in_nats(b, c) - (double)b * c.inv_tau_d + log((double)r.sum);
+    const double log_unit = c.teacher.lse ? base_in_nats(top, c) - (double)c.teacher.lse[row] : -log(mass);
+    const double unit = c.teacher.lse ? exp(log_unit) : 1.0 / mass;
+    const bool left_out = teacher.sum == 0.f;
+    if (c.loss) c.loss[row] = left_out ? 0.f : (float)(c.scale * (double)weight * unit * (cross * c.inv_tau_d + mass * (log_unit - slip_of_top + rest)));
+    if (c.lse) c.lse[row] = left_out ? 0.f : (float)((double)b * c.inv_tau_d + rest);
+}
+
+// What the CTAs of a cluster tell one another and the warps of a CTA theirs: running sums of the student's and of the teacher's row.
+struct Joint {
+    Running student, teacher;
 };
 
 // FORWARD: the sum over the row is computed (else it is `kept`); GRAD: the gradient is written.
 template <typename T, bool FORWARD, bool GRAD>
-__global__ void __launch_bounds__(THREADS, 2) distill_kernel(const Call c, const T* logits, T* grad) {
-    constexpr int W = 16 / (int)sizeof(T), U = 4;
-    __shared__ int32_t s_id[TOP];
-    __shared__ float s_p[TOP], s_at[TOP];  // exp(z / tau - largest), the student's logit
-    __shared__ int32_t table[TABLE];
-    __shared__ double s_d[WARPS];
-    __shared__ float s_f[WARPS];
-    __shared__ float2 s_part[WARPS + 1];
-    const uint32_t rank = cluster_rank(), size = cluster_size();
-    const int64_t row = blockIdx.x / size;
+__global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) distill_kernel(const Call c, const T* logits, T* grad) {
+    constexpr int W = 16 / (int)sizeof(T), U = 4, PAIRS = Unit<T>::PAIRS;
+    extern __shared__ __align__(16) uint4 copy[];  // [room]; unit u of a round in place u, thread u % THREADS
+    int32_t* const s_id = reinterpret_cast<int32_t*>(copy + c.room);  // [top]
+    float *const s_z = reinterpret_cast<float*>(s_id + c.top), *const s_at = s_z + c.top;  // [top] the teacher's logit, the student's
+    uint16_t* const table = reinterpret_cast<uint16_t*>(s_at + c.top);  // [1 << log_slots]
+    __shared__ Joint s_warp[WARPS];
+    __shared__ float2 s_cta[8];
+    __shared__ int s_again;
+    const uint32_t rank = cluster_rank(), size = 1u << c.log_cluster;
+    const int64_t row = blockIdx.x >> c.log_cluster;
     const int tid = threadIdx.x;
     const T* const s = logits + row * c.ldl;
     T* const g = GRAD ? grad + row * c.ldg : nullptr;
     const float weight = c.row_weights ? c.row_weights[row] : 1.f;
     const int64_t e0 = c.rows.begin(row), entries = max((int64_t)0, c.rows.end(row) - e0);
-    const bool few = entries <= TOP;
+    const bool few = entries <= c.top;
+    const Share mine = share_of(s, c.n, rank, c.log_cluster);
+    const int rounds = mine.units <= c.room ? (mine.units > 0) : (mine.units + c.room - 1) / c.room;
+    const bool aligned = !GRAD || reinterpret_cast<uintptr_t>(g + mine.head) % 16 == 0;
+    const int64_t last = mine.first + (int64_t)mine.units * W;
+    auto is_mine = [&](int64_t id) { return (id >= mine.first && id < last) || (rank == 0 && (id < mine.head || id >= mine.tail)); };
 
-    // the teacher's row: largest logit, sum of exponentials
-    float top = -CUDART_INF_F;
-    bool any = false;  // an id of the vocabulary with a logit other than -infinity
-    if (weight != 0.f) {
-        for (int64_t t = tid; t < entries; t += THREADS) {
-            const int32_t id = c.teacher.ids[e0 + t];
-            const bool held = id >= 0 && id < c.n;
-            const float z = held ? c.teacher.logit(e0 + t) : -CUDART_INF_F;
-            any |= z != -CUDART_INF_F;
-            top = fmaxf(top, z);
-            if (few) {
-                s_id[t] = held ? id : -1;
-                s_p[t] = z;
-                s_at[t] = held ? widen(s[id]) : 0.f;
-            }
-        }
-    }
-    const bool live = __syncthreads_or(any);
-    const Share mine = share_of(s, c.n, rank, size);
-    if (!live) {  // (the same for the whole cluster)
-        if (tid == 0 && rank == 0 && FORWARD) {
+    auto leave_out = [&] {  // (the same for the whole cluster)
+        if (FORWARD && tid == 0 && rank == 0) {
             if (c.loss) c.loss[row] = 0.f;
             if (c.lse) c.lse[row] = 0.f;
         }
         if (GRAD) {
-            const int64_t w0 = rank == 0 ? 0 : mine.head + mine.v0 * W, w1 = mine.head + mine.v1 * W;
-            for (int64_t v = w0 + tid; v < w1; v += THREADS) g[v] = narrow<T>(0.f);
-            if (rank == 0)
-                for (int64_t v = mine.tail + tid; v < c.n; v += THREADS) g[v] = narrow<T>(0.f);
+            if (aligned) {
+                for (int u = tid; u < mine.units; u += THREADS) *reinterpret_cast<uint4*>(g + mine.first + (int64_t)u * W) = uint4{0, 0, 0, 0};
+            } else {
+                for (int64_t v = mine.first + tid; v < last; v += THREADS) g[v] = narrow<T>(0.f);
+            }
+            if (rank == 0) {
+                if (tid < mine.head) g[tid] = narrow<T>(0.f);
+                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(0.f);
+            }
         }
+    };
+    if (weight == 0.f || entries == 0) {
+        leave_out();
         return;
     }
-    top = base_of(over_cta(top, s_f, [](float a, float b) { return fmaxf(a, b); }));
-    double total = 0;  // sum of e_t = exp((z_t - top) / tau)
+
+    if (size > 1) cluster_arrive_relaxed();  // (shared memory of a CTA that has not begun is nobody's to write to)
+
+    // a round's units: two groups of copies, so that the first half can be used while the second is under way
+    const int half = c.room / 2;
+    auto fetch = [&](int round) {
+        const int count = min(c.room, mine.units - round * c.room);
+        const T* const from = s + mine.first + (int64_t)round * c.room * W;
+        for (int u = tid; u < min(count, half); u += THREADS) copy_unit(copy + u, from + (int64_t)u * W);
+        copies_issued();
+        for (int u = half + tid; u < count; u += THREADS) copy_unit(copy + u, from + (int64_t)u * W);
+        copies_issued();
+    };
+    if (rounds > 0 && (FORWARD || few)) fetch(0);
+
+    // the teacher's row while the copies are under way
+    Running teacher{-CUDART_INF_F, 0.f};
     for (int64_t t = tid; t < entries; t += THREADS) {
-        float e = 0.f;
+        const int32_t id = c.teacher.ids[e0 + t];
+        const bool held = id >= 0 && id < c.n;
+        const float z[1] = {held ? c.teacher.logit(e0 + t) : -CUDART_INF_F};
         if (few) {
-            if (s_id[t] >= 0) e = expf((s_p[t] - top) * c.inv_tau);
-            s_p[t] = e;
-        } else {
-            const int32_t id = c.teacher.ids[e0 + t];
-            if (id >= 0 && id < c.n) e = expf((c.teacher.logit(e0 + t) - top) * c.inv_tau);
+            s_id[t] = held ? id : -1;
+            s_z[t] = z[0];
+            s_at[t] = held && (rank == 0 || is_mine(id)) ? widen(s[id]) : 0.f;
         }
-        total += (double)e;
+        take<1>(teacher, z, c.k);
     }
-    const auto sum = [](double a, double b) { return a + b; };
-    total = over_cta(total, s_d, sum);
-    // p_t = e_t * unit, mass P
-    const double log_unit = c.teacher.lse ? (double)top * c.inv_tau_d - (double)c.teacher.lse[row] : -log(total);
-    const double unit = c.teacher.lse ? exp(log_unit) : 1.0 / total;
-    const double mass = c.teacher.lse ? total * unit : total / total;  // (1, or NaN)
+    const int slots = 1 << c.log_slots;
+    constexpr uint16_t NO_ENTRY = 0xffff;
+    if (GRAD && few) {
+        for (int i = tid; i < slots; i += THREADS) table[i] = NO_ENTRY;
+        if (tid == 0) s_again = 0;
+    }
 
     Running r{-CUDART_INF_F, 0.f};
-    double lse;
     if (FORWARD) {
-        for (int64_t v = mine.v0 + tid; v < mine.v1; v += (int64_t)U * THREADS) {
-            Vec<T, W> x[U];
+        for (int round = 0; round < rounds; ++round) {
+            if (round > 0) fetch(round);  // (a thread overwrites what it has used itself)
+            const int count = min(c.room, mine.units - round * c.room);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (v + u * THREADS < mine.v1) x[u] = *reinterpret_cast<const Vec<T, W>*>(s + mine.head + (v + u * THREADS) * W);
+            for (int part = 0; part < 2; ++part) {
+                if (part == 0) wait_copies<1>(); else wait_copies<0>();
+                const int to = part == 0 ? min(count, half) : count;
+                for (int u0 = part * half + tid; u0 < to; u0 += U * THREADS) {
+                    uint4 x[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (v + u * THREADS >= mine.v1) break;
-                float f[W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) f[i] = widen(x[u].x[i]);
-                take<W>(r, f, c.k);
+                    for (int i = 0; i < U; ++i) {
+                        constexpr uint32_t none = Unit<T>::NOTHING;
+                        x[i] = u0 + i * THREADS < to ? copy[u0 + i * THREADS] : uint4{none, none, none, none};
+                    }
+                    take_units<T, U>(r, x, c.k);
+                }
             }
         }
         if (rank == 0) {
@@ -223,162 +441,190 @@ __global__ void __launch_bounds__(THREADS, 2) distill_kernel(const Call c, const
                 take<1>(r, f, c.k);
             }
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) r = merge(r, Running{__shfl_xor_sync(FULL_MASK, r.most, o), __shfl_xor_sync(FULL_MASK, r.sum, o)}, c.k);
-        if (lane_id() == 0) s_part[tid >> 5] = float2{r.most, r.sum};
-        __syncthreads();
-        r = Running{s_part[0].x, s_part[0].y};
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) r = merge(r, Running{s_part[w].x, s_part[w].y}, c.k);
-        if (size > 1) {
-            if (tid == 0) s_part[WARPS] = float2{r.most, r.sum};
-            cluster_sync();
-            const float2 first = load_of_rank(s_part + WARPS, 0);
-            r = Running{first.x, first.y};
-            for (uint32_t q = 1; q < size; ++q) {
-                const float2 other = load_of_rank(s_part + WARPS, q);
-                r = merge(r, Running{other.x, other.y}, c.k);
-            }
-        }
-        // log q = (s - b) / tau - rest.  (k is rounded, 1 / tau is not: what the rounding moves b k by is put back.)
-        const float b = base_of(r.most);
-        const double slip = fabsf(b) < LARGE ? (double)__fmul_rn(b, c.k) - (double)b * (double)c.k : 0.0;
-        const double rest = slip * LN2 + log((double)r.sum);
-        lse = (double)b * c.inv_tau_d + rest;
-        if (rank == 0) {
-            double loss = 0;
-            for (int64_t t = tid; t < entries; t += THREADS) {
-                const int32_t id = few ? s_id[t] : c.teacher.ids[e0 + t];
-                if (id < 0 || id >= c.n) continue;
-                const float z = c.teacher.logit(e0 + t), at = few ? s_at[t] : widen(s[id]);
-                const float e = few ? s_p[t] : expf((z - top) * c.inv_tau);
-                if (e != 0.f) loss += (double)e * ((((double)z - (double)top) - ((double)at - (double)b)) * c.inv_tau_d + log_unit + rest);
-            }
-            loss = over_cta(loss, s_d, sum);
-            if (tid == 0) {
-                if (c.loss) c.loss[row] = (float)(c.scale * (double)weight * (loss * unit));
-                if (c.lse) c.lse[row] = (float)lse;
-            }
-        }
-        if (size > 1) cluster_sync();  // nobody ends, or overwrites logits, before all have read
-    } else {
-        lse = (double)c.kept[row];
-        if (size > 1) cluster_sync();  // nobody overwrites logits before all have fetched the teacher's
     }
-    if (!GRAD) return;
+    // joined over the warp, the CTA, the cluster
+    if (FORWARD) r = join<32>(r, c.k);
+    if ((tid & ~31) < entries) teacher = join<32>(teacher, c.k);
+    if (lane_id() == 0) s_warp[tid >> 5] = Joint{r, teacher};
+    __syncthreads();
+    const Joint joint = s_warp[lane_id() & (WARPS - 1)];
+    if (FORWARD) r = join<WARPS>(joint.student, c.k);
+    teacher = join<WARPS>(joint.teacher, c.k);
+    if (size > 1) {
+        cluster_wait();
+        if (FORWARD && tid < size) store_to_rank(s_cta + rank, float2{r.most, r.sum}, tid);
+        cluster_arrive();
+    }
 
-    // G_v = a 2^(s k - shift) - (at the teacher's ids) f * (sum of their e_t); what rounding the shift takes away goes into a.  The
-    // shift that belongs to a kept lse is that of a logit with q = 1, so that the rounding of k matters to small q only.
-    const double factor = c.scale * (double)weight * c.inv_tau_d;
-    const float b = FORWARD ? base_of(r.most) : 0.f;
-    const bool plain = fabsf(b) < LARGE;
-    // a row that was NaN or -infinity throughout is NaN in all places
-    const bool sound = FORWARD ? r.sum > 0.f && r.sum < CUDART_INF_F : fabs(lse) < (double)LARGE;
-    const double exact = !sound ? (double)CUDART_NAN_F
-                         : FORWARD ? (plain ? (double)__fmul_rn(b, c.k) : 0.0) + log2((double)r.sum) : lse / c.inv_tau_d * (double)c.k;
-    const float shift = (float)exact;
-    const float a = (float)(factor * mass * exp2((double)shift - exact)), f = (float)(factor * unit);
-    auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k - shift); };
-    if (few) {
-        for (int64_t v = mine.v0 + tid; v < mine.v1; v += (int64_t)U * THREADS) {
-            Vec<T, W> x[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (v + u * THREADS < mine.v1) x[u] = *reinterpret_cast<const Vec<T, W>*>(s + mine.head + (v + u * THREADS) * W);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (v + u * THREADS >= mine.v1) break;
-                float y[W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) y[i] = a * q_of(widen(x[u].x[i]));
-                T* const at = g + mine.head + (v + u * THREADS) * W;
-                if (reinterpret_cast<uintptr_t>(at) % 16 == 0) {
-                    store_narrow<T, W>(at, W, y);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) at[i] = narrow<T>(y[i]);
-                }
-            }
-        }
-        if (rank == 0) {
-            if (tid < mine.head) g[tid] = narrow<T>(a * q_of(widen(s[tid])));
-            if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(a * q_of(widen(s[mine.tail + tid])));
-        }
-        // the first entry of every id: slots of the table hold entries, an id's slot its first
-        for (int i = tid; i < TABLE; i += THREADS) table[i] = NONE;
-        __syncthreads();
-        const int count = (int)entries;
-        auto slot_of = [](int32_t id) { return (int)(((uint32_t)id * 2654435761u) >> 21); };
-        static_assert(TABLE == 1 << 11, "slot_of");
-        bool again = false;
-        for (int t = tid; t < count; t += THREADS) {
+    // meanwhile: an entry for every id of the share; slots of the table hold entries, one of an id's
+    const int count = (int)min(entries, (int64_t)c.top);
+    uint32_t chosen = 0;  // a bit for each of this thread's entries
+    static_assert(MOST_TOP / THREADS <= 32, "bits");
+    if (GRAD && few) {
+        for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {
             const int32_t id = s_id[t];
-            if (id < 0) continue;
-            for (int q = slot_of(id);; q = (q + 1) & (TABLE - 1)) {  // (the table is at most half full)
-                const int was = atomicCAS(&table[q], NONE, t);
-                if (was == NONE) break;
+            if (id < 0 || !is_mine(id)) continue;
+            for (int q = (int)(((uint32_t)id * 2654435761u)   >> (32 - c.log_slots));; q = (q + 1) & (slots - 1)) {  // (multiplicative hashing; at most half full)
+                const uint16_t was = atomicCAS(&table[q], NO_ENTRY, (uint16_t)t);
+                if (was == NO_ENTRY) {
+                    chosen |= 1u << bit;
+                    break;
+                }
                 if (s_id[was] == id) {
-                    atomicMin(&table[q], t);
-                    again = true;
+                    s_again = 1;
                     break;
                 }
             }
         }
-        again = __syncthreads_or(again);
-        const int64_t w0 = rank == 0 ? 0 : mine.head + mine.v0 * W, w1 = mine.head + mine.v1 * W;
-        for (int t = tid; t < count; t += THREADS) {
-            const int32_t id = s_id[t];
-            if (id < 0 || !((id >= w0 && id < w1) || (rank == 0 && id >= mine.tail))) continue;
-            float e = s_p[t];
-            if (again) {
-                int q = slot_of(id);
-                while (s_id[table[q]] != id) q = (q + 1) & (TABLE - 1);
-                if (table[q] != t) continue;
-                for (int o = t + 1; o < count; ++o)
-                    if (s_id[o] == id) e += s_p[o];
-            }
-            g[id] = narrow<T>(fmaf(-e, f, a * q_of(s_at[t])));
+    }
+    // p_t = e_t * unit with e_t as in teacher.sum, mass P
+    const float top = base_of(teacher.most);
+    const float unit = c.teacher.lse ? expf((float)(base_in_nats(top, c) - (double)c.teacher.lse[row])) : 1.f / teacher.sum;
+    const float mass = c.teacher.lse ? teacher.sum * unit : 1.f + 0.f * teacher.sum;  // (1, or NaN)
+    auto e_of = [&](float z) { return term(z, top, c.k); };
+
+    if (size > 1) {
+        cluster_wait();  // from here on logits may be overwritten: all have fetched the teacher's
+        if (FORWARD) {
+            const float2 part = s_cta[lane_id() & (size - 1)];
+            r = Running{part.x, part.y};
+            r = size == 2 ? join<2>(r, c.k) : size == 4 ? join<4>(r, c.k) : join<8>(r, c.k);
         }
+    }
+    if (!few && FORWARD) {  // the loss needs logits that the gradient may overwrite
+        if (rank == 0) write_loss(c, row, weight, e0, entries, false, s_id, s_z, s_at, s, r, top, teacher);
+        if (size > 1) {
+            cluster_arrive();
+            cluster_wait();
+        }
+    }
+    if (teacher.sum == 0.f) {  // no entry with a logit other than -infinity
+        wait_copies<0>();
+        leave_out();
         return;
     }
-    // Rows of many entries: windows of TABLE ids, in every window the first entry of each id by its place.
-    for (int64_t i0 = 0; i0 < c.n; i0 += TABLE) {
-        const int64_t i1 = min(i0 + TABLE, c.n);
-        if ((i0 / TABLE) % size != rank) continue;
-        for (int i = tid; i < TABLE; i += THREADS) table[i] = NONE;
-        if (tid == 0) s_id[0] = 0;
-        __syncthreads();
-        for (int64_t t = tid; t < entries; t += THREADS) {
-            const int32_t id = c.teacher.ids[e0 + t];
-            if (id < i0 || id >= i1) continue;
-            if (atomicMin(&table[id - i0], (int)t) != NONE) s_id[0] = 1;
+    if (GRAD) {
+        // G_v = a 2^(s k - shift) - (at the teacher's ids) f e; a row that was NaN or -infinity throughout is NaN in all places.  The shift that
+        // belongs to a kept lse is that of a logit with q = 1, so that the rounding of k matters to small q only; what
+        // rounding the shift takes away goes into a (its logarithm is below 2^-15: two terms of the exponential's series are exact to 2^-45).
+        const float factor = c.factor * weight, f = factor * unit;
+        float a, shift, b = 0.f;
+        if (FORWARD) {
+            b = base_of(r.most);
+            shift = fabsf(b) < LARGE ? __fmul_rn(b, c.k) : 0.f;
+            a = r.sum > 0.f && r.sum < CUDART_INF_F ? factor * mass / r.sum : CUDART_NAN_F;
+        } else {
+            const double lse = (double)c.kept[row], exact = lse / c.inv_tau_d * (double)c.k;
+            shift = (float)exact;
+            const double slip = ((double)shift - exact) * LN2;
+            a = fabs(lse) < (double)LARGE ? (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip)) : CUDART_NAN_F;
         }
-        __syncthreads();
-        const bool again = s_id[0] != 0;
-        for (int64_t v = i0 + tid; v < i1; v += THREADS) {
-            float y = a * q_of(widen(s[v]));
-            const int first = table[v - i0];
-            if (first != NONE) {
-                float e = 0.f;
-                for (int64_t t = first; t < (again ? entries : first + 1); ++t)
-                    if (c.teacher.ids[e0 + t] == v) e += expf((c.teacher.logit(e0 + t) - top) * c.inv_tau);
-                y = fmaf(-e, f, y);
+        const bool plain = fabsf(b) < LARGE;
+        auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
+        if (few) {
+            for (int i = 0; i < rounds; ++i) {
+                // what the sum has left in shared memory first
+                const int round = FORWARD ? (i == 0 ? rounds - 1 : i - 1) : i;
+                if (i > 0) fetch(round);
+                wait_copies<0>();
+                const int units = min(c.room, mine.units - round * c.room);
+                T* const to = g + mine.first + (int64_t)round * c.room * W;
+                if (plain && aligned) {
+                    const Pair kk = pair(c.k, c.k), off = pair(-shift, -shift), aa = pair(a, a);
+#pragma unroll 4
+                    for (int u = tid; u < units; u += THREADS) {
+                        const uint4 x = copy[u];
+                        float2 y[PAIRS];
+#pragma unroll
+                        for (int q = 0; q < PAIRS; ++q) {
+                            const float2 p = halves(multiply_add(Unit<T>::get(x, q), kk, off));
+                            y[q] = halves(multiply(pair(power_of_two(p.x), power_of_two(p.y)), aa));
+                        }
+                        *reinterpret_cast<uint4*>(to + (int64_t)u * W) = Unit<T>::put(y);
+                    }
+                } else {
+                    for (int u = tid; u < units; u += THREADS) {
+                        const Vec<T, W> x = *reinterpret_cast<const Vec<T, W>*>(copy + u);
+#pragma unroll
+                        for (int q = 0; q < W; ++q) to[(int64_t)u * W + q] = narrow<T>(a * q_of(widen(x.x[q])));
+                    }
+                }
             }
-            g[v] = narrow<T>(y);
+            if (rank == 0) {
+                if (tid < mine.head) g[tid] = narrow<T>(a * q_of(widen(s[tid])));
+                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(a * q_of(widen(s[mine.tail + tid])));
+            }
+            __syncthreads();
+            const bool again = s_again != 0;
+            for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {
+                if (!(chosen >> bit & 1u)) continue;
+                const int32_t id = s_id[t];
+                float e = e_of(s_z[t]);
+                if (again) {
+                    e = 0.f;
+                    for (int o = 0; o < count; ++o)
+                        if (s_id[o] == id) e += e_of(s_z[o]);
+                }
+                g[id] = narrow<T>(fmaf(-e, f, a * q_of(s_at[t])));
+            }
+        } else {
+            // Rows of many entries: windows of ids, in every window the first entry of each id by its place.
+            wait_copies<0>();
+            int32_t* const firsts = reinterpret_cast<int32_t*>(copy);
+            for (int64_t i0 = (int64_t)rank * WINDOW; i0 < c.n; i0 += (int64_t)size * WINDOW) {
+                const int64_t i1 = min(i0 + WINDOW, c.n);
+                __syncthreads();
+                for (int i = tid; i < WINDOW; i += THREADS) firsts[i] = NONE;
+                if (tid == 0) s_again = 0;
+                __syncthreads();
+                for (int64_t t = tid; t < entries; t += THREADS) {
+                    const int32_t id = c.teacher.ids[e0 + t];
+                    if (id < i0 || id >= i1) continue;
+                    if (atomicMin(&firsts[id - i0], (int)t) != NONE) s_again = 1;
+                }
+                __syncthreads();
+                const bool again = s_again != 0;
+                for (int64_t v = i0 + tid; v < i1; v += THREADS) {
+                    float y = a * q_of(widen(s[v]));
+                    const int first = firsts[v - i0];
+                    if (first != NONE) {
+                        float e = 0.f;
+                        for (int64_t t = first; t < (again ? entries : first + 1); ++t)
+                            if (c.teacher.ids[e0 + t] == v) e += e_of(c.teacher.logit(e0 + t));
+                        y = fmaf(-e, f, y);
+                    }
+                    g[v] = narrow<T>(y);
+                }
+            }
         }
-        __syncthreads();
     }
+    if (FORWARD && few && rank == 0) write_loss(c, row, weight, e0, entries, true, s_id, s_z, s_at, s, r, top, teacher);
 }
 
 template <typename T, bool FORWARD, bool GRAD>
-spsyrk_status_t launch(const Call& c, const void* logits, void* grad, cudaStream_t st) {
-    // as many CTAs per row as two CTAs per SM need, each with at least 8192 logits
+spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    constexpr auto kernel = distill_kernel<T, FORWARD, GRAD>;
+    const int64_t units = (c.n + W - 1) / W;
+    // shares of at most DISTILL_SHARE bytes; smaller ones, down to 16 KB, as long as the CTAs do not fill the GPU
     int cluster = 1;
-    while (cluster < 8 && c.rows.m * cluster < 2 * SMS && c.n / (2 * cluster) >= 8192) cluster *= 2;
+    while (cluster < 8 && (units > cluster * (DISTILL_SHARE / 16) || (c.rows.m * cluster < 3 * SMS && units >= cluster * 1024))) cluster *= 2, ++c.log_cluster;
     if (c.rows.m * cluster >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
+    // entries in shared memory: all if every row has as many, else room for four times the mean
+    const int64_t entries = c.rows.rowptr ? std::max<int64_t>(128, 4 * (c.rows.nnz / c.rows.m)) : c.rows.k;
+    c.top = LEAST_TOP;
+    c.log_slots = 6;
+    while (c.top < entries && c.top < MOST_TOP) c.top *= 2, ++c.log_slots;
+    static_assert(LEAST_TOP == 32, "log_slots");
+    const size_t kept = (size_t)c.top * 12 + (GRAD ? (size_t)2 << c.log_slots : 0);
+    const int64_t share = std::max<int64_t>((units + cluster - 1) / cluster, FEWEST_UNITS);
+    constexpr int STEP = 2 * THREADS;
+    c.room = (int)((std::min<int64_t>(share, 200 * 1024 / 16) + STEP - 1) / STEP * STEP);
+    SPSYRK_CUDA_TRY(allow_shared_memory<kernel>());
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(c.rows.m * cluster));
     cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)c.room * 16 + kept;
     cfg.stream = st;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -386,7 +632,7 @@ spsyrk_status_t launch(const Call& c, const void* logits, void* grad, cudaStream
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    SPSYRK_CUDA_TRY(launch_kernel(cfg, distill_kernel<T, FORWARD, GRAD>, Call(c), static_cast<const T*>(logits), static_cast<T*>(grad)));
+    SPSYRK_CUDA_TRY(launch_kernel(cfg, kernel, Call(c), static_cast<const T*>(logits), static_cast<T*>(grad)));
     return SPSYRK_OK;
 }
 
@@ -414,6 +660,8 @@ spsyrk_status_t distill(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype,
     c.inv_tau = (float)(1.0 / temperature);
     c.inv_tau_d = 1.0 / temperature;
     c.scale = scale;
+    c.factor = (float)(scale / temperature);
+    c.log_cluster = 0;
     c.ldl = ldl;
     c.ldg = ldg;
     c.loss = d_loss;

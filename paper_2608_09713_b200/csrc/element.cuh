@@ -100,8 +100,13 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
+// (relaxed: says only that this CTA has come so far)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive;\nbarrier.cluster.wait;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 __device__ __forceinline__ uint32_t address_in(const void* mine, uint32_t rank) {
     uint32_t there;
@@ -118,10 +123,8 @@ __device__ __forceinline__ double load_of_rank(const double* mine, uint32_t rank
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(address_in(mine, rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ float2 load_of_rank(const float2* mine, uint32_t rank) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(address_in(mine, rank)) : "memory");
-    return v;
+__device__ __forceinline__ void store_to_rank(const float2* mine, float2 v, uint32_t rank) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(address_in(mine, rank)), "f"(v.x), "f"(v.y) : "memory");
 }
 
 }  // namespace spsyrk
