@@ -3,11 +3,12 @@
 //     loss = scale r sum_t p_t (log p_t - log q_{id_t}),      G_v = scale r / tau (P q_v - sum of the p_t with id v).
 //
 // Bound by memory: the logits are read once and the gradient is written once.  A cluster of 1 to 8 CTAs takes a row, each a contiguous
-// share of it, which is copied to shared memory (cp.async, every thread the 16-byte units that it will use itself, so that nobody waits
-// for anybody) while the teacher's entries are looked at; a running maximum and sum per thread, joined over the CTA and the cluster; then the
-// gradient from the copies.  (Reading the row a second time instead finds it in L2 only in part: 296 rows of 256 KB and their gradients
-// are more than L2 holds; 605 us for 4096 rows of 131072 bfloat16 logits, 160 us for a quarter of them at an L2 hit rate of 9 %.)
-// A share that shared memory does not hold goes through it in rounds.
+// share of it: a running maximum and sum per thread, joined over the CTA and the cluster, then the gradient, for which the share is read
+// again.  It is then still in L2 as long as the shares under way are a fraction of it (888 of 64 KB, 57 MB; with rows of 256 KB a CTA, 76 MB and as
+// much of gradients, a third of the reads went to memory again).  A CTA lives some 13 us, most of them latencies, so what counts is how many bytes
+// are under way: six CTAs per SM, and one instruction that asks for the whole share to be brought to L2 before the teacher's entries are
+// looked at (422 us without it, 389 with it for 4096 rows of 131072 bfloat16 logits, 2.1 GB: 84 % of the copy rate).  Kept in shared memory instead
+// of L2 only three shares fit an SM (513 us; with CTAs that stay and copy the next row meanwhile 660, whose rows wait for one another).
 // exp(x) is computed as 2^(s * log2(e) / tau - ...): a multiply-add (two logits per instruction) and an exponential per logit.
 // The gradient is first written for all ids as if they were not the teacher's, then the few of the teacher's are overwritten, from
 // logits that were fetched beforehand (so the gradient may overwrite the logits).  An id that occurs more than once is written for one
@@ -26,7 +27,19 @@ namespace {
 #define DISTILL_THREADS 256
 #endif
 #ifndef DISTILL_WARPS_PER_SM
-#define DISTILL_WARPS_PER_SM 24
+#define DISTILL_WARPS_PER_SM 48
+#endif
+#ifndef DISTILL_PREFETCH
+#define DISTILL_PREFETCH 1
+#endif
+#ifndef DISTILL_SHARE1
+#define DISTILL_SHARE1 131072
+#endif
+#ifndef DISTILL_LD2
+#define DISTILL_LD2 __ldcg
+#endif
+#ifndef DISTILL_U
+#define DISTILL_U 4
 #endif
 #ifndef DISTILL_SHARE
 #define DISTILL_SHARE 65536
@@ -36,7 +49,6 @@ constexpr int WARPS = THREADS / 32;
 constexpr int MOST_TOP = 1024;    // teacher's entries of a row that are kept in shared memory, at most
 constexpr int LEAST_TOP = 32;
 constexpr int WINDOW = 2048;      // ids of a window in rows of more entries
-constexpr int FEWEST_UNITS = WINDOW * 4 / 16;  // 16-byte units of the copy: the windows' table takes its place
 constexpr int SMS = 148;
 constexpr int NONE = 0x7fffffff;
 constexpr double LOG2E = 1.4426950408889634, LN2 = 0.6931471805599453;
@@ -236,12 +248,10 @@ __device__ __forceinline__ void take_units(Running& r, const uint4 (&u)[U], floa
     }
 }
 
-__device__ __forceinline__ void copy_unit(void* to, const void* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+// Asks for bytes that will be read soon to be brought to L2; address and number of bytes are multiples of 16.
+__device__ __forceinline__ void prefetch(const void* from, int bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int PENDING>
-__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
 // A row's columns in 16-byte units from its first 16-byte boundary: this CTA has `units` of them from column `first` on, and the
 // first CTA also the `head` columns before the boundary and those from `tail` on, behind the last unit.
@@ -274,7 +284,6 @@ struct Call {
     float factor;       // scale / tau
     int log_cluster;    // CTAs of a row
     int top, log_slots; // entries that are kept in shared memory; slots of the hash table, at least twice as many
-    int room;           // units that the copy in shared memory holds, a multiple of 2 * THREADS
 };
 
 // What the terms of a running sum are taken relative to, as a logarithm.  (k is rounded, 1 / tau is not: base / tau, and what rounding
@@ -332,9 +341,9 @@ struct Joint {
 // FORWARD: the sum over the row is computed (else it is `kept`); GRAD: the gradient is written.
 template <typename T, bool FORWARD, bool GRAD>
 __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) distill_kernel(const Call c, const T* logits, T* grad) {
-    constexpr int W = 16 / (int)sizeof(T), U = 4, PAIRS = Unit<T>::PAIRS;
-    extern __shared__ __align__(16) uint4 copy[];  // [room]; unit u of a round in place u, thread u % THREADS
-    int32_t* const s_id = reinterpret_cast<int32_t*>(copy + c.room);  // [top]
+    constexpr int W = 16 / (int)sizeof(T), U = DISTILL_U, PAIRS = Unit<T>::PAIRS;
+    extern __shared__ int32_t windows[];  // rows of many entries: [WINDOW]; else the teacher's entries
+    int32_t* const s_id = windows;  // [top]
     float *const s_z = reinterpret_cast<float*>(s_id + c.top), *const s_at = s_z + c.top;  // [top] the teacher's logit, the student's
     uint16_t* const table = reinterpret_cast<uint16_t*>(s_at + c.top);  // [1 << log_slots]
     __shared__ Joint s_warp[WARPS];
@@ -349,7 +358,6 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
     const int64_t e0 = c.rows.begin(row), entries = max((int64_t)0, c.rows.end(row) - e0);
     const bool few = entries <= c.top;
     const Share mine = share_of(s, c.n, rank, c.log_cluster);
-    const int rounds = mine.units <= c.room ? (mine.units > 0) : (mine.units + c.room - 1) / c.room;
     const bool aligned = !GRAD || reinterpret_cast<uintptr_t>(g + mine.head) % 16 == 0;
     const int64_t last = mine.first + (int64_t)mine.units * W;
     auto is_mine = [&](int64_t id) { return (id >= mine.first && id < last) || (rank == 0 && (id < mine.head || id >= mine.tail)); };
@@ -376,21 +384,11 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         return;
     }
 
-    if (size > 1) cluster_arrive_relaxed();  // (shared memory of a CTA that has not begun is nobody's to write to)
+    if (size > 1) cluster_arrive();  // (shared memory of a CTA that has not begun is nobody's to write to)
 
-    // a round's units: two groups of copies, so that the first half can be used while the second is under way
-    const int half = c.room / 2;
-    auto fetch = [&](int round) {
-        const int count = min(c.room, mine.units - round * c.room);
-        const T* const from = s + mine.first + (int64_t)round * c.room * W;
-        for (int u = tid; u < min(count, half); u += THREADS) copy_unit(copy + u, from + (int64_t)u * W);
-        copies_issued();
-        for (int u = half + tid; u < count; u += THREADS) copy_unit(copy + u, from + (int64_t)u * W);
-        copies_issued();
-    };
-    if (rounds > 0 && (FORWARD || few)) fetch(0);
+    if (DISTILL_PREFETCH && tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, mine.units * 16);
 
-    // the teacher's row while the copies are under way
+    // the teacher's row
     Running teacher{-CUDART_INF_F, 0.f};
     for (int64_t t = tid; t < entries; t += THREADS) {
         const int32_t id = c.teacher.ids[e0 + t];
@@ -412,23 +410,16 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
 
     Running r{-CUDART_INF_F, 0.f};
     if (FORWARD) {
-        for (int round = 0; round < rounds; ++round) {
-            if (round > 0) fetch(round);  // (a thread overwrites what it has used itself)
-            const int count = min(c.room, mine.units - round * c.room);
+        const uint4* const from = reinterpret_cast<const uint4*>(s + mine.first);
+        for (int u0 = tid; u0 < mine.units; u0 += U * THREADS) {
+            uint4 x[U];
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                if (part == 0) wait_copies<1>(); else wait_copies<0>();
-                const int to = part == 0 ? min(count, half) : count;
-                for (int u0 = part * half + tid; u0 < to; u0 += U * THREADS) {
-                    uint4 x[U];
-#pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        constexpr uint32_t none = Unit<T>::NOTHING;
-                        x[i] = u0 + i * THREADS < to ? copy[u0 + i * THREADS] : uint4{none, none, none, none};
-                    }
-                    take_units<T, U>(r, x, c.k);
-                }
+            for (int i = 0; i < U; ++i) {
+                constexpr uint32_t none = Unit<T>::NOTHING;
+                x[i] = uint4{none, none, none, none};
+                if (u0 + i * THREADS < mine.units) x[i] = __ldcg(from + u0 + i * THREADS);
             }
+            take_units<T, U>(r, x, c.k);
         }
         if (rank == 0) {
             float f[1];
@@ -499,7 +490,6 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         }
     }
     if (teacher.sum == 0.f) {  // no entry with a logit other than -infinity
-        wait_copies<0>();
         leave_out();
         return;
     }
@@ -522,29 +512,32 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         const bool plain = fabsf(b) < LARGE;
         auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
         if (few) {
-            for (int i = 0; i < rounds; ++i) {
-                // what the sum has left in shared memory first
-                const int round = FORWARD ? (i == 0 ? rounds - 1 : i - 1) : i;
-                if (i > 0) fetch(round);
-                wait_copies<0>();
-                const int units = min(c.room, mine.units - round * c.room);
-                T* const to = g + mine.first + (int64_t)round * c.room * W;
+            {
+                const uint4* const from = reinterpret_cast<const uint4*>(s + mine.first);
+                T* const to = g + mine.first;
+                const int units = mine.units;
                 if (plain && aligned) {
                     const Pair kk = pair(c.k, c.k), off = pair(-shift, -shift), aa = pair(a, a);
-#pragma unroll 4
-                    for (int u = tid; u < units; u += THREADS) {
-                        const uint4 x = copy[u];
-                        float2 y[PAIRS];
+                    for (int u0 = tid; u0 < units; u0 += U * THREADS) {
+                        uint4 x[U];
 #pragma unroll
-                        for (int q = 0; q < PAIRS; ++q) {
-                            const float2 p = halves(multiply_add(Unit<T>::get(x, q), kk, off));
-                            y[q] = halves(multiply(pair(power_of_two(p.x), power_of_two(p.y)), aa));
+                        for (int i = 0; i < U; ++i)
+                            if (u0 + i * THREADS < units) x[i] = DISTILL_LD2(from + u0 + i * THREADS);
+#pragma unroll
+                        for (int i = 0; i < U; ++i) {
+                            if (u0 + i * THREADS >= units) break;
+                            float2 y[PAIRS];
+#pragma unroll
+                            for (int q = 0; q < PAIRS; ++q) {
+                                const float2 p = halves(multiply_add(Unit<T>::get(x[i], q), kk, off));
+                                y[q] = halves(multiply(pair(power_of_two(p.x), power_of_two(p.y)), aa));
+                            }
+                            __stcs(reinterpret_cast<uint4*>(to + (int64_t)(u0 + i * THREADS) * W), Unit<T>::put(y));
                         }
-                        *reinterpret_cast<uint4*>(to + (int64_t)u * W) = Unit<T>::put(y);
                     }
                 } else {
                     for (int u = tid; u < units; u += THREADS) {
-                        const Vec<T, W> x = *reinterpret_cast<const Vec<T, W>*>(copy + u);
+                        const Vec<T, W> x = *reinterpret_cast<const Vec<T, W>*>(from + u);
 #pragma unroll
                         for (int q = 0; q < W; ++q) to[(int64_t)u * W + q] = narrow<T>(a * q_of(widen(x.x[q])));
                     }
@@ -569,8 +562,7 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
             }
         } else {
             // Rows of many entries: windows of ids, in every window the first entry of each id by its place.
-            wait_copies<0>();
-            int32_t* const firsts = reinterpret_cast<int32_t*>(copy);
+            int32_t* const firsts = windows;
             for (int64_t i0 = (int64_t)rank * WINDOW; i0 < c.n; i0 += (int64_t)size * WINDOW) {
                 const int64_t i1 = min(i0 + WINDOW, c.n);
                 __syncthreads();
@@ -608,7 +600,7 @@ spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) 
     const int64_t units = (c.n + W - 1) / W;
     // shares of at most DISTILL_SHARE bytes; smaller ones, down to 16 KB, as long as the CTAs do not fill the GPU
     int cluster = 1;
-    while (cluster < 8 && (units > cluster * (DISTILL_SHARE / 16) || (c.rows.m * cluster < 3 * SMS && units >= cluster * 1024))) cluster *= 2, ++c.log_cluster;
+    while (cluster < 8 && (units > cluster * ((FORWARD && GRAD ? DISTILL_SHARE : DISTILL_SHARE1) / 16) || (c.rows.m * cluster < 3 * SMS && units >= cluster * 1024))) cluster *= 2, ++c.log_cluster;
     if (c.rows.m * cluster >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
     // entries in shared memory: all if every row has as many, else room for four times the mean
     const int64_t entries = c.rows.rowptr ? std::max<int64_t>(128, 4 * (c.rows.nnz / c.rows.m)) : c.rows.k;
@@ -617,14 +609,11 @@ spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) 
     while (c.top < entries && c.top < MOST_TOP) c.top *= 2, ++c.log_slots;
     static_assert(LEAST_TOP == 32, "log_slots");
     const size_t kept = (size_t)c.top * 12 + (GRAD ? (size_t)2 << c.log_slots : 0);
-    const int64_t share = std::max<int64_t>((units + cluster - 1) / cluster, FEWEST_UNITS);
-    constexpr int STEP = 2 * THREADS;
-    c.room = (int)((std::min<int64_t>(share, 200 * 1024 / 16) + STEP - 1) / STEP * STEP);
     SPSYRK_CUDA_TRY(allow_shared_memory<kernel>());
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(c.rows.m * cluster));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = (size_t)c.room * 16 + kept;
+    cfg.dynamicSmemBytes = std::max<size_t>(kept, GRAD ? WINDOW * 4 : 0);
     cfg.stream = st;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;

@@ -100,8 +100,6 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-// (relaxed: says only that this CTA has come so far)
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
@@ -123,6 +121,33 @@ __device__ __forceinline__ double load_of_rank(const double* mine, uint32_t rank
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(address_in(mine, rank)) : "memory");
     return v;
 }
+
+// A barrier in shared memory that counts bytes: every use of it (a phase) ends when `expect` has named the bytes and they have arrived.
+__device__ __forceinline__ void barrier_init(uint64_t* bar) {
+    asm volatile("mbarrier.init.shared.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar)) : "memory");
+}
+__device__ __forceinline__ void barrier_init_visible() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar)), "r"(bytes) : "memory");
+}
+// Waits for the end of a phase; false if the wait ran out.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, uint32_t parity) {
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(bar);
+    for (int polls = 0; polls < (1 << 20); ++polls) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(at), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+// v into another CTA's shared memory, where 8 bytes more have then arrived.  Unlike a barrier of the cluster this does not wait for
+// what has been stored to global memory before.
+__device__ __forceinline__ void store_to_rank(const float2* mine, float2 v, uint64_t* bar, uint32_t rank) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address_in(mine, rank)), "f"(v.x), "f"(v.y),
+                 "r"(address_in(bar, rank))
+                 : "memory");
+}
+
 __device__ __forceinline__ void store_to_rank(const float2* mine, float2 v, uint32_t rank) {
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(address_in(mine, rank)), "f"(v.x), "f"(v.y) : "memory");
 }
