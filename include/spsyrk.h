@@ -397,7 +397,7 @@ spsyrk_status_t spsyrk_plan_set_jaccard(spsyrk_plan_t plan, float *d_jaccard);
  * F64 and in single precision otherwise, in an order that depends on sizes and alignment only, and rounded once: the same call gives the
  * same bits.  All of these calls are asynchronous and can be captured into a graph.
  * Common errors: INVALID_ARG (a null pointer with something to read or write behind it, a negative size, a stride below the row's
- * length, nnz not a multiple of m without row pointers, a type that is not listed), OVERFLOW (m, n or nnz >= 2^31 - 1, p > 2^22), CUDA.
+ * length, nnz not a multiple of m without row pointers, a type that is not listed), OVERFLOW (m, n or nnz >= 2^31 - 1, p > 2^21), CUDA.
  */
 
 /*

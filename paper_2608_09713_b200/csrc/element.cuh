@@ -31,6 +31,18 @@ struct alignas(sizeof(T) * W) Vec {
 };
 template <typename T, int V> constexpr int VEC_OF = V * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : V;
 
+// the first `left` elements at p as they are, zeros behind them
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> load_raw(const T* __restrict__ p, int64_t left) {
+    Vec<T, V> v;
+    if (left >= V) {
+        v = *reinterpret_cast<const Vec<T, V>*>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v.x[i] = i < left ? p[i] : T(0.f);
+    }
+    return v;
+}
 // the first `left` elements at p, widened, zeros behind them
 template <typename T, int V>
 __device__ __forceinline__ void load_wide(const T* __restrict__ p, int64_t left, typename Wide<T>::type (&x)[V]) {
@@ -84,6 +96,17 @@ struct Rows {
         while (lo < hi) {
             const int64_t mid = (lo + hi + 1) >> 1;
             if (rowptr[mid] <= e) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    }
+    // the same by a whole warp, among all rows: 32 of them looked at per step
+    __device__ __forceinline__ int64_t row_of_by_warp(int64_t e) const {
+        int64_t lo = 0, hi = m - 1;
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 31) / 32, at = lo + (lane_id() + 1) * step;
+            const int before = __popc(__ballot_sync(FULL_MASK, at <= hi && rowptr[at] <= e));
+            lo += before * step;
+            hi = min(hi, lo + step - 1);
         }
         return lo;
     }

@@ -23,82 +23,81 @@ int group_shift(int64_t vectors) {
     return s;
 }
 
-// One id a row.  A group copies U rows, so that U loads of a lane are under way at a time.
-template <typename T, int V, int U>
+// One id a row, a group per row.  (Four rows per group, for four loads of a lane under way at a time, took 60 us instead of 47 for 20011 rows
+// of 4096 bfloat16: as many CTAs with fewer registers hide more.)
+template <typename T, int V>
 __global__ void __launch_bounds__(THREADS) lookup_one_kernel(int64_t m, int64_t n, int64_t p, const int32_t* __restrict__ ids,
                                                              const typename Wide<T>::type* __restrict__ weights, typename Wide<T>::type scale,
                                                              const T* __restrict__ e, int64_t lde, T* __restrict__ y, int64_t ldy, int shift) {
     using A = typename Wide<T>::type;
-    const int64_t group = (int64_t)blockIdx.x * (THREADS >> shift) + (threadIdx.x >> shift);
-    const int64_t groups = (int64_t)gridDim.x * (THREADS >> shift);
+    const int64_t r = (int64_t)blockIdx.x * (THREADS >> shift) + (threadIdx.x >> shift);
     const int lane = threadIdx.x & ((1 << shift) - 1);
-    int64_t id[U];
-    A w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t r = group + u * groups;
-        id[u] = r < m ? ids[r] : -1;
-        w[u] = r < m && weights ? weights[r] * scale : scale;
-    }
+    if (r >= m) return;
+    const int64_t id = ids[r];
+    const bool held = id >= 0 && id < n;
+    const A w = held && weights ? weights[r] * scale : scale;
     for (int64_t c = (int64_t)lane * V; c < p; c += (int64_t)V << shift) {
-        A x[U][V];
+        A x[V] = {};
+        if (held) {
+            load_wide<T, V>(e + id * lde + c, p - c, x);
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_wide<T, V>(e + (id[u] >= 0 && id[u] < n ? id[u] * lde + c : 0), id[u] >= 0 && id[u] < n ? p - c : 0, x[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t r = group + u * groups;
-            if (r >= m) continue;
-            if (id[u] >= 0 && id[u] < n) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[u][i] *= w[u];
-            }
-            store_narrow<T, V>(y + r * ldy + c, p - c, x[u]);
+            for (int i = 0; i < V; ++i) x[i] *= w;
         }
+        store_narrow<T, V>(y + r * ldy + c, p - c, x);
     }
 }
 
-// acc += the weighted rows of entries [b, e) at column c, eight rows under way at a time
+// acc += the weighted rows of entries [b, end) at column c, UNROLL rows under way at a time.  The lanes of a group (those of it that
+// share a warp) fetch an id and a weight each and hand them round; the next ones are under way meanwhile.
+constexpr int UNROLL = 8;
 template <typename T, int V>
-__device__ __forceinline__ void add_entries(int64_t b, int64_t e_end, int64_t n, int64_t p, int64_t c, const int32_t* __restrict__ ids,
-                                            const typename Wide<T>::type* __restrict__ weights, const T* __restrict__ e, int64_t lde,
+__device__ __forceinline__ void add_entries(int64_t b, int64_t end, int64_t n, int64_t p, int64_t c, const int32_t* __restrict__ ids,
+                                            const typename Wide<T>::type* __restrict__ weights, const T* __restrict__ e, int64_t lde, int shift,
                                             typename Wide<T>::type (&acc)[V]) {
     using A = typename Wide<T>::type;
-    constexpr int U = V * (int)sizeof(T) >= 16 && sizeof(T) <= 4 ? 8 : 4;
-    for (int64_t t = b; t < e_end; t += U) {
-        int64_t id[U];
-        A w[U];
+    constexpr int U = UNROLL;
+    const int share = 1 << min(shift, 5), lane = threadIdx.x & (share - 1);
+    const unsigned mask = share == 32 ? FULL_MASK : ((1u << share) - 1) << (lane_id() & ~(share - 1));
+    int32_t next_id = -1;
+    A next_w = A(1);
+    auto ask = [&](int64_t t) {
+        next_id = t + lane < end ? ids[t + lane] : -1;
+        if (weights) next_w = t + lane < end ? weights[t + lane] : A(0);
+    };
+    ask(b);
+    for (int64_t t = b; t < end; t += share) {
+        const int32_t my_id = next_id >= 0 && next_id < n ? next_id : -1;
+        const A my_w = next_w;
+        ask(t + share);
+        const int count = (int)min((int64_t)share, end - t);
+        for (int k = 0; k < count; k += U) {
+            int32_t id[U];
+            Vec<T, V> x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            id[u] = t + u < e_end ? ids[t + u] : -1;
-            w[u] = weights && t + u < e_end ? weights[t + u] : A(1);
-        }
-        Vec<T, V> x[U];
-        const bool whole = p - c >= V;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (id[u] < 0 || id[u] >= n) continue;
-            const T* at = e + id[u] * lde + c;
-            if (whole) {
-                x[u] = *reinterpret_cast<const Vec<T, V>*>(at);
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (c + i < p) x[u].x[i] = at[i];
+            for (int u = 0; u < U; ++u) {
+                // (a lane beyond the group's gives an id of the group again)
+                const int32_t got = __shfl_sync(mask, my_id, k + u, share);
+                id[u] = k + u < count ? got : -1;
             }
-        }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (id[u] < 0 || id[u] >= n) continue;
+            for (int u = 0; u < U; ++u) {
+                if (id[u] < 0) continue;
+                x[u] = load_raw<T, V>(e + id[u] * lde + c, p - c);
+            }
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < p) acc[i] += w[u] * widen(x[u].x[i]);
+            for (int u = 0; u < U; ++u) {
+                const A w = weights ? __shfl_sync(mask, my_w, k + u, share) : A(1);
+                if (id[u] < 0) continue;
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += w * widen(x[u].x[i]);
+            }
         }
     }
 }
 
 // A group per row; rows of more than `longest` entries are left to lookup_long_kernel.
 template <typename T, int V>
-__global__ void __launch_bounds__(THREADS) lookup_rows_kernel(Rows a, int64_t n, int64_t p, const int32_t* __restrict__ ids,
+__global__ void __launch_bounds__(THREADS, 3) lookup_rows_kernel(Rows a, int64_t n, int64_t p, const int32_t* __restrict__ ids,
                                                               const typename Wide<T>::type* __restrict__ weights, typename Wide<T>::type scale,
                                                               const T* __restrict__ e, int64_t lde, T* __restrict__ y, int64_t ldy, int shift,
                                                               int64_t longest) {
@@ -109,12 +108,14 @@ __global__ void __launch_bounds__(THREADS) lookup_rows_kernel(Rows a, int64_t n,
     if (row < a.m) {
         const int64_t b = a.begin(row), end = a.end(row);
         if (end - b <= longest) {
-            for (int64_t c = (int64_t)lane * V; c < p; c += (int64_t)V << shift) {
+            // (all lanes of a group stay together: they hand ids round)
+            for (int64_t c0 = 0; c0 < p; c0 += (int64_t)V << shift) {
+                const int64_t c = c0 + (int64_t)lane * V;
                 A acc[V] = {};
-                add_entries<T, V>(b, end, n, p, c, ids, weights, e, lde, acc);
+                add_entries<T, V>(b, end, n, p, c, ids, weights, e, lde, shift, acc);
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] *= scale;
-                store_narrow<T, V>(y + row * ldy + c, p - c, acc);
+                if (c < p) store_narrow<T, V>(y + row * ldy + c, p - c, acc);
             }
         }
     }
@@ -159,7 +160,7 @@ __global__ void __cluster_dims__(LONG_CLUSTER, 1, 1) __launch_bounds__(THREADS)
             const int64_t share = (len + (int64_t)LONG_CLUSTER * groups - 1) / ((int64_t)LONG_CLUSTER * groups);
             const int64_t mine = min(len, (rank * (int64_t)groups + group) * share);
             A acc[V] = {};
-            if (c < p) add_entries<T, V>(b + mine, b + min(len, mine + share), n, p, c, ids, weights, e, lde, acc);
+            add_entries<T, V>(b + mine, b + min(len, mine + share), n, p, c, ids, weights, e, lde, shift, acc);
 #pragma unroll
             for (int i = 0; i < V; ++i) part[i * THREADS + threadIdx.x] = acc[i];
             __syncthreads();
@@ -186,47 +187,91 @@ __global__ void __cluster_dims__(LONG_CLUSTER, 1, 1) __launch_bounds__(THREADS)
     chain_end(blockIdx.x == 0 && blockIdx.y == 0);
 }
 
-// A CTA takes DW_ENTRIES entries, a group of at most 32 lanes four of them at a time; rows are looked for between the CTA's
-// first and last one.
-constexpr int DW_EACH = 4;
+// A group of up to 32 lanes takes `each` consecutive entries, DW_EACH of them at a time.  Every lane fetches an id and looks for its
+// row (between the CTA's first and last one) and hands them round.  Entries of the same row share the loads of dY.
+constexpr int DW_EACH = 8;
 template <typename T, int V>
-__global__ void __launch_bounds__(THREADS) lookup_grad_weights_kernel(Rows a, int64_t n, int64_t p, const int32_t* __restrict__ ids,
+__global__ void __launch_bounds__(THREADS, 3) lookup_grad_weights_kernel(Rows a, int64_t n, int64_t p, const int32_t* __restrict__ ids,
                                                                       typename Wide<T>::type scale, const T* __restrict__ e, int64_t lde,
                                                                       const T* __restrict__ dy, int64_t lddy,
-                                                                      typename Wide<T>::type* __restrict__ dw, int shift) {
+                                                                      typename Wide<T>::type* __restrict__ dw, int shift, int each) {
     using A = typename Wide<T>::type;
     __shared__ int64_t span[2];
     const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
-    const int64_t here = (int64_t)(THREADS >> shift) * DW_EACH, base = (int64_t)blockIdx.x * here;
+    const unsigned mask = lanes == 32 ? FULL_MASK : ((1u << lanes) - 1) << (lane_id() & ~(lanes - 1));
+    const int64_t here = (int64_t)(THREADS >> shift) * each, base = (int64_t)blockIdx.x * here;
     if (a.rowptr) {
-        if (threadIdx.x < 2) span[threadIdx.x] = a.row_of(threadIdx.x == 0 ? base : min(base + here, a.nnz) - 1, 0, a.m - 1);
+        if (threadIdx.x < 64) {
+            const int64_t r = a.row_of_by_warp(threadIdx.x < 32 ? base : min(base + here, a.nnz) - 1);
+            if (lane_id() == 0) span[threadIdx.x >> 5] = r;
+        }
         __syncthreads();
     }
-    const int64_t t0 = base + (int64_t)(threadIdx.x >> shift) * DW_EACH;
-    const T *row[DW_EACH], *line[DW_EACH];
-    A dot[DW_EACH] = {};
+    const int64_t t0 = base + (int64_t)(threadIdx.x >> shift) * each, t1 = min(t0 + each, a.nnz);
+    for (int64_t t = t0; t < t1; t += lanes) {
+        int32_t my_id = t + lane < t1 ? ids[t + lane] : -1, my_row = 0;
+        if (my_id >= n || (my_id >= 0 && !a.covered(t + lane))) my_id = -1;
+        if (my_id >= 0) my_row = (int32_t)(a.rowptr ? a.row_of(t + lane, span[0], span[1]) : (t + lane) / a.k);
+        for (int k = 0; k < lanes && t + k < t1; k += DW_EACH) {
+            int32_t id[DW_EACH], row[DW_EACH];
+            A dot[DW_EACH] = {};
+            bool same = true;  // all of one row, or padding
+            int32_t the_row = -1;
 #pragma unroll
-    for (int u = 0; u < DW_EACH; ++u) {
-        const int64_t t = t0 + u, id = t < a.nnz ? ids[t] : -1;
-        line[u] = id >= 0 && id < n && a.covered(t) ? e + id * lde : nullptr;
-        row[u] = line[u] ? dy + (a.rowptr ? a.row_of(t, span[0], span[1]) : t / a.k) * lddy : nullptr;
-    }
-    for (int64_t c = (int64_t)lane * V; c < p; c += (int64_t)V << shift) {
-        A x[DW_EACH][V], g[DW_EACH][V];
+            for (int u = 0; u < DW_EACH; ++u) {
+                const int32_t got = __shfl_sync(mask, my_id, k + u, lanes);
+                row[u] = __shfl_sync(mask, my_row, k + u, lanes);
+                id[u] = k + u < lanes ? got : -1;
+                if (id[u] >= 0) {
+                    same &= the_row < 0 || the_row == row[u];
+                    the_row = row[u];
+                }
+            }
+            if (the_row >= 0) {
+                for (int64_t c = (int64_t)lane * V; c < p; c += (int64_t)V << shift) {
+                    A g[V];
+                    Vec<T, V> x[DW_EACH];
 #pragma unroll
-        for (int u = 0; u < DW_EACH; ++u) {
-            load_wide<T, V>(line[u] ? line[u] + c : e, line[u] ? p - c : 0, x[u]);
-            load_wide<T, V>(row[u] ? row[u] + c : dy, row[u] ? p - c : 0, g[u]);
+                    for (int u = 0; u < DW_EACH; ++u)
+                        if (id[u] >= 0) x[u] = load_raw<T, V>(e + id[u] * lde + c, p - c);
+                    if (same) load_wide<T, V>(dy + the_row * lddy + c, p - c, g);
+#pragma unroll
+                    for (int u = 0; u < DW_EACH; ++u) {
+                        if (!same) load_wide<T, V>(id[u] >= 0 ? dy + row[u] * lddy + c : dy, id[u] >= 0 ? p - c : 0, g);
+                        if (id[u] < 0) continue;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) dot[u] += widen(x[u].x[i]) * g[i];
+                    }
+                }
+            }
+            // every dot product over the lanes; with eight lanes or more a step halves what a lane holds
+            int place = 0;
+            if (lanes >= DW_EACH) {
+#pragma unroll
+                for (int s = 0; s < 5; ++s) {
+                    if (1 << s >= lanes) break;
+                    const bool upper = lane >> s & 1;
+                    const int half = DW_EACH >> (s + 1);
+                    if (half > 0) {
+#pragma unroll
+                        for (int i = 0; i < half; ++i) {
+                            const A keep = upper ? dot[i + half] : dot[i], give = upper ? dot[i] : dot[i + half];
+                            dot[i] = keep + __shfl_xor_sync(mask, give, 1 << s);
+                        }
+                        place += upper ? half : 0;
+                    } else {
+                        dot[0] += __shfl_xor_sync(mask, dot[0], 1 << s);
+                    }
+                }
+                if (lane < DW_EACH && t + k + place < t1) dw[t + k + place] = dot[0] * scale;
+            } else {
+#pragma unroll
+                for (int u = 0; u < DW_EACH; ++u) {
+                    for (int o = lanes >> 1; o > 0; o >>= 1) dot[u] += __shfl_xor_sync(mask, dot[u], o);
+                    if (lane == 0 && k + u < lanes && t + k + u < t1) dw[t + k + u] = dot[u] * scale;
+                }
+            }
         }
-#pragma unroll
-        for (int u = 0; u < DW_EACH; ++u)
-#pragma unroll
-            for (int i = 0; i < V; ++i) dot[u] += x[u][i] * g[u][i];
-    }
-#pragma unroll
-    for (int u = 0; u < DW_EACH; ++u) {
-        for (int o = lanes >> 1; o > 0; o >>= 1) dot[u] += __shfl_xor_sync(FULL_MASK, dot[u], o);
-        if (lane == 0 && t0 + u < a.nnz) dw[t0 + u] = line[u] ? dot[u] * scale : A(0);
     }
 }
 
@@ -240,12 +285,7 @@ spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t*
     const int shift = group_shift((p + V - 1) / V);
     const int64_t per_cta = THREADS >> shift;
     if (!a.rowptr && a.k == 1) {
-        // four rows a group once every SM has its 2048 threads twice over; fewer rows are spread as far as they go
-        const bool many = a.m >= 4 * 2 * SMS * 2048 / (1 << shift);
-        const int64_t groups = many ? (a.m + 3) / 4 : a.m;
-        const unsigned ctas = (unsigned)((groups + per_cta - 1) / per_cta);
-        if (many) lookup_one_kernel<T, V, 4><<<ctas, THREADS, 0, st>>>(a.m, n, p, ids, wv, (A)scale, ev, lde, yv, ldy, shift);
-        else lookup_one_kernel<T, V, 1><<<ctas, THREADS, 0, st>>>(a.m, n, p, ids, wv, (A)scale, ev, lde, yv, ldy, shift);
+        lookup_one_kernel<T, V><<<(unsigned)((a.m + per_cta - 1) / per_cta), THREADS, 0, st>>>(a.m, n, p, ids, wv, (A)scale, ev, lde, yv, ldy, shift);
         note_launches(1);
         SPSYRK_CUDA_TRY(cudaGetLastError());
         return SPSYRK_OK;
@@ -281,9 +321,12 @@ spsyrk_status_t grad_weights_typed(const Rows& a, int64_t n, int64_t p, const in
                                    int64_t lddy, void* dw, cudaStream_t st) {
     using A = typename Wide<T>::type;
     const int shift = std::min(group_shift((p + V - 1) / V), 5);
-    const int64_t here = (int64_t)(THREADS >> shift) * DW_EACH;
+    // 32 entries a group if their groups still fill every SM with threads, down to 8 if not
+    int each = 32;
+    while (each > DW_EACH && (a.nnz / each << shift) < (int64_t)SMS * 2048) each /= 2;
+    const int64_t here = (int64_t)(THREADS >> shift) * each;
     lookup_grad_weights_kernel<T, V><<<(unsigned)((a.nnz + here - 1) / here), THREADS, 0, st>>>(a, n, p, ids, (A)scale, static_cast<const T*>(e), lde,
-                                                                                                static_cast<const T*>(dy), lddy, static_cast<A*>(dw), shift);
+                                                                                                static_cast<const T*>(dy), lddy, static_cast<A*>(dw), shift, each);
     note_launches(1);
     SPSYRK_CUDA_TRY(cudaGetLastError());
     return SPSYRK_OK;
@@ -293,7 +336,7 @@ spsyrk_status_t grad_weights_typed(const Rows& a, int64_t n, int64_t p, const in
 spsyrk_status_t check_rows(int64_t m, int64_t n, int64_t p, int64_t nnz, const int64_t* d_rowptr, const int32_t* d_ids, Rows* rows) {
     if (m < 0 || n < 0 || p < 0 || nnz < 0 || (nnz > 0 && !d_ids)) return SPSYRK_ERR_INVALID_ARG;
     constexpr int64_t most = (int64_t(1) << 31) - 1;
-    if (m >= most || n >= most || nnz >= most || p > (int64_t(1) << 22)) return SPSYRK_ERR_OVERFLOW;
+    if (m >= most || n >= most || nnz >= most || p > (int64_t(1) << 21)) return SPSYRK_ERR_OVERFLOW;
     if (!d_rowptr && (m == 0 ? nnz != 0 : nnz % m != 0)) return SPSYRK_ERR_INVALID_ARG;
     *rows = Rows{d_rowptr, m, nnz, m > 0 ? nnz / m : 0};
     return SPSYRK_OK;

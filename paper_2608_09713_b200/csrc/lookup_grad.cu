@@ -2,10 +2,11 @@
 //
 // The entries are ordered by id with a stable sort (entries of an id stay in their order), and the ordered list is cut into pieces of
 // the same length.  A group of lanes adds up a piece, 16 bytes of dY a lane, run by run (a run = the entries of one id): a run that lies
-// inside the piece is written to its row of dE at once, one that crosses the piece's ends leaves its partial sum in the workspace, and
-// the partial sums of such a run are added up in their order by a second kernel.  No atomic adds: the same call gives the same bits,
-// and an id that every second entry has costs no more than others.  Rows of ids that do not occur are filled with zeros by further
-// CTAs, which find them in a bit per id that is set while the ids are read.
+// inside the piece is written to its row of dE at once, one that crosses the piece's ends leaves its partial sum in the workspace.  The
+// partial sums of such runs are joined in their order, 64 pieces at a time, then 64 times 64, until one block holds them all.  No atomic
+// adds: the same call gives the same bits, and an id that every tenth entry has costs no more than others (joined by one CTA
+// its 5500 pieces of 64 columns took 270 us).  Rows of ids that do not occur are filled with zeros by CTAs that go along with the sort,
+// which leaves the memory idle.
 // Bound by memory: dY is read once (a row of several ids once per id, through L2), dE written once.
 #include <algorithm>
 
@@ -30,11 +31,16 @@ int piece_of(int64_t nnz, int64_t p) {
     return c;
 }
 
+constexpr int JOIN = 64;        // pieces (blocks of pieces) that are joined at a time
+constexpr int JOIN_LEVELS = 6;  // 2^31 entries in pieces of MIN_PIECE: 2^29, 2^23, 2^17, 2^11, 2^5, 1
+
 struct GradWs {
     uint32_t *key[2], *row[2];  // ids (n: padding) and rows of the entries, before and after a pass
     void* weight[2];
     uint32_t* present;  // a bit per id
-    void* part;         // [pieces][2][p] partial sums: of a run that comes from the piece before, of one that begins here and goes on
+    // [pieces][2][p] partial sums: of a run that comes from the piece before, of one that begins here and goes on; then those of blocks of
+    // JOIN pieces, of JOIN times JOIN, down to a single one
+    void* part[JOIN_LEVELS];
     RadixState rs;
     uint32_t* err;
     void* zero;
@@ -58,7 +64,11 @@ size_t carve(GradWs* w, void* ws, int64_t n, int64_t p, int64_t nnz, bool wide, 
         t.weight[i] = weighted ? take(ne * acc) : nullptr;
     }
     const int piece = piece_of(nnz, p);
-    t.part = take((size_t)((ne + piece - 1) / piece) * 2 * p * acc);
+    int64_t count = (ne + piece - 1) / piece;
+    for (int level = 0; level < JOIN_LEVELS; ++level) {
+        t.part[level] = count > 1 ? take((size_t)count * 2 * p * acc) : nullptr;
+        count = (count + JOIN - 1) / JOIN;
+    }
     // what has to be zero at the start, in one piece
     const size_t bits = ((size_t)n / 32 + 1) * 4 / 8 * 8 + 8;
     const size_t words = nnz > FEW ? radix_state_words(radix_tiles(nnz), radix_wide(nnz), radix_passes((uint64_t)n)) : 0;
@@ -74,68 +84,154 @@ size_t carve(GradWs* w, void* ws, int64_t n, int64_t p, int64_t nnz, bool wide, 
     return (off + ALIGN - 1) / ALIGN * ALIGN;
 }
 
-// Key and row of every entry, a bit per id that occurs and, for the sort, the sizes of all digits.
+// Zeros for the rows [v0, v1) of dE without entries.  A warp takes up to 32 rows, every lane looks for one of them whether it has entries;
+// then up to a warp per row: elements up to the first 16-byte boundary, 16 bytes a lane, the elements behind.
+struct Fill {
+    char* de;
+    int64_t row_bytes, used_bytes;  // from row to row; of a row
+    int size;                       // of an element
+    int64_t rows;                   // a CTA's
+    int64_t n;
+    template <typename Present>
+    __device__ __forceinline__ void rows_of(int64_t v0, int64_t v1, Present present) const {
+        const int shift = min(5, 32 - __clz((int)min((used_bytes + 15) / 16, (int64_t)32) - 1));
+        const int lanes = 1 << shift, lane = lane_id() & (lanes - 1), warps = blockDim.x >> 5;
+        const int each = (int)min((int64_t)32, (v1 - v0 + warps - 1) / warps);
+        for (int64_t first = v0 + (int64_t)(threadIdx.x >> 5) * each; first < v1; first += (int64_t)warps * each) {
+            const int count = (int)min((int64_t)each, v1 - first);
+            const unsigned taken = __ballot_sync(FULL_MASK, lane_id() < count && present(first + lane_id()));
+            for (int r = lane_id() >> shift; r < count; r += 32 >> shift) {
+                if (taken >> r & 1u) continue;
+                char* const at = de + (first + r) * row_bytes;
+                const int64_t head = min(used_bytes, (int64_t)((0 - reinterpret_cast<uintptr_t>(at)) % 16)), body = (used_bytes - head) / 16;
+                const int64_t tail = head + body * 16;
+                if (head > 0) zeros(at, head, lane, lanes);
+                for (int64_t c = lane; c < body; c += lanes) reinterpret_cast<uint4*>(at + head)[c] = uint4{0, 0, 0, 0};
+                if (tail < used_bytes) zeros(at + tail, used_bytes - tail, lane, lanes);
+            }
+        }
+    }
+    __device__ __forceinline__ void zeros(char* at, int64_t bytes, int lane, int lanes) const {
+        for (int64_t c = (int64_t)lane * size; c < bytes; c += (int64_t)lanes * size) {
+            if (size == 2) *reinterpret_cast<uint16_t*>(at + c) = 0;
+            else if (size == 4) *reinterpret_cast<uint32_t*>(at + c) = 0;
+            else *reinterpret_cast<uint64_t*>(at + c) = 0;
+        }
+    }
+};
+
+// Key and row of every entry, a bit per id that occurs and the sizes of all digits.
 constexpr int READ_ITEMS = 4;
-constexpr int READ_CHUNK = THREADS * READ_ITEMS;
+constexpr int READ_CHUNK = THREADS * READ_ITEMS;  // a step of a CTA
 __global__ void __launch_bounds__(THREADS) read_ids_kernel(Rows a, int64_t n, const int32_t* __restrict__ ids, uint32_t* __restrict__ key,
-                                                           uint32_t* __restrict__ row, uint32_t* __restrict__ present, int passes,
+                                                           uint32_t* __restrict__ row, uint32_t* present, int passes,
                                                            unsigned long long* __restrict__ bins) {
     __shared__ int64_t span[2];
     __shared__ uint32_t h[RX_MAX_PASSES][RX_BINS];
     for (int d = threadIdx.x; d < RX_MAX_PASSES * RX_BINS; d += THREADS) (&h[0][0])[d] = 0;
-    const int64_t base = (int64_t)blockIdx.x * READ_CHUNK;
-    if (a.rowptr && threadIdx.x < 2) span[threadIdx.x] = a.row_of(threadIdx.x == 0 ? base : min(base + READ_CHUNK, a.nnz) - 1, 0, a.m - 1);
-    __syncthreads();
+    for (int64_t base = (int64_t)blockIdx.x * READ_CHUNK; base < a.nnz; base += (int64_t)gridDim.x * READ_CHUNK) {
+        __syncthreads();
+        if (a.rowptr && threadIdx.x < 64) {
+            const int64_t r = a.row_of_by_warp(threadIdx.x < 32 ? base : min(base + READ_CHUNK, a.nnz) - 1);
+            if (lane_id() == 0) span[threadIdx.x >> 5] = r;
+        }
+        __syncthreads();
+        uint32_t k[READ_ITEMS];
+        uint32_t seen[READ_ITEMS];
 #pragma unroll
-    for (int i = 0; i < READ_ITEMS; ++i) {
-        const int64_t t = base + i * THREADS + threadIdx.x;
-        if (t >= a.nnz) continue;
-        const int64_t id = ids[t], r = a.rowptr ? a.row_of(t, span[0], span[1]) : t / a.k;
-        const bool held = id >= 0 && id < n && a.covered(t);
-        const uint32_t k = held ? (uint32_t)id : (uint32_t)n;
-        key[t] = k;
-        row[t] = (uint32_t)r;
-        if (held) atomicOr(present + (k >> 5), 1u << (k & 31));
-        for (int q = 0; q < passes; ++q) atomicAdd(&h[q][(k >> (q * RX_BITS)) & (RX_BINS - 1)], 1u);
+        for (int i = 0; i < READ_ITEMS; ++i) {
+            const int64_t t = base + i * THREADS + threadIdx.x, id = t < a.nnz ? ids[t] : -1;
+            k[i] = id >= 0 && id < n && a.covered(t) ? (uint32_t)id : (uint32_t)n;
+        }
+        // (looked at first: an id that every tenth of 2 million entries has took 100 us of atomic operations on one word)
+#pragma unroll
+        for (int i = 0; i < READ_ITEMS; ++i) seen[i] = __ldcg(present + (k[i] >> 5));
+#pragma unroll
+        for (int i = 0; i < READ_ITEMS; ++i) {
+            const int64_t t = base + i * THREADS + threadIdx.x;
+            if (t >= a.nnz) continue;
+            key[t] = k[i];
+            row[t] = (uint32_t)(a.rowptr ? a.row_of(t, span[0], span[1]) : t / a.k);
+            if (k[i] < (uint32_t)n && !(seen[i] >> (k[i] & 31) & 1u)) atomicOr(present + (k[i] >> 5), 1u << (k[i] & 31));
+            for (int q = 0; q < passes; ++q) atomicAdd(&h[q][(k[i] >> (q * RX_BITS)) & (RX_BINS - 1)], 1u);
+        }
     }
     __syncthreads();
     for (int d = threadIdx.x; d < passes * RX_BINS; d += THREADS)
         if ((&h[0][0])[d]) atomicAdd(&bins[d], (unsigned long long)(&h[0][0])[d]);
 }
 
-// Up to FEW entries: an entry's place in the order is the number of entries with a smaller id, or with the same one before it.  A
-// warp counts for four entries at a time.
+// A share of the rows, as work that goes along with a radix pass.
+struct FillWithPass {
+    static constexpr bool IS_SOME = true;
+    Fill fill;
+    const uint32_t* present;
+    int64_t begin, end;
+    unsigned ctas() const { return (unsigned)((end - begin + fill.rows - 1) / fill.rows); }
+    __device__ __forceinline__ void operator()(int64_t cta) const {
+        const int64_t v0 = begin + cta * fill.rows;
+        fill.rows_of(v0, min(v0 + fill.rows, end), [&](int64_t v) { return (__ldcg(present + (v >> 5)) >> (v & 31) & 1u) != 0; });
+    }
+};
+
+// Up to FEW entries: an entry's place in the order is the number of entries with a smaller id, or with the same one before it.  All
+// keys are fetched to shared memory, and a warp counts for four entries at a time, 128 keys a step.  CTAs behind those of the entries fill rows: they
+// look the ids through for those of their rows.
 constexpr int RANK_EACH = 4;
+constexpr int RANK_HERE = THREADS / 32 * RANK_EACH;  // entries of a CTA
+constexpr int FILL_MOST = FEW * 32;                  // rows of a CTA that fills: a bit each in the place of the keys
 template <typename A>
 __global__ void __launch_bounds__(THREADS) rank_kernel(Rows a, int64_t n, const int32_t* __restrict__ ids, const A* __restrict__ weights,
-                                                       uint32_t* __restrict__ key, uint32_t* __restrict__ row, A* __restrict__ weight,
-                                                       uint32_t* __restrict__ present) {
-    const int lane = lane_id();
-    const int nnz = (int)a.nnz, t0 = (int)(blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * RANK_EACH;
+                                                       uint32_t* __restrict__ key, uint32_t* __restrict__ row, A* __restrict__ weight, int rank_ctas,
+                                                       Fill fill) {
+    __shared__ __align__(16) uint32_t keys[FEW];
+    const int nnz = (int)a.nnz, lane = lane_id();
     const int64_t from = a.rowptr ? a.rowptr[0] : 0, to = a.rowptr ? a.rowptr[a.m] : a.nnz;
     auto key_of = [&](int t) {
         const int64_t id = ids[t];
         return id >= 0 && id < n && t >= from && t < to ? (uint32_t)id : (uint32_t)n;
     };
+    if ((int)blockIdx.x >= rank_ctas) {
+        const int64_t v0 = ((int64_t)blockIdx.x - rank_ctas) * fill.rows, v1 = min(v0 + fill.rows, n);
+        for (int i = threadIdx.x; i < (int)((v1 - v0 + 31) / 32); i += THREADS) keys[i] = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (int t = threadIdx.x; t < nnz; t += THREADS) {
+            const int64_t k = key_of(t);
+            if (k >= v0 && k < v1) atomicOr(&keys[(k - v0) >> 5], 1u << ((k - v0) & 31));
+        }
+        __syncthreads();
+        fill.rows_of(v0, v1, [&](int64_t v) { return (keys[(v - v0) >> 5] >> ((v - v0) & 31) & 1u) != 0; });
+        return;
+    }
+    const int up = (nnz + 127) / 128 * 128;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < up; t += THREADS) keys[t] = t < nnz ? key_of(t) : NO_KEY;  // (behind all others)
+    const int t0 = (int)(blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * RANK_EACH;
+    const int64_t my_row = lane < RANK_EACH && t0 + lane < nnz ? a.row_of(t0 + lane, 0, a.m - 1) : 0;  // (while the keys are under way)
+    __syncthreads();
+    if (t0 >= nnz) return;
     uint32_t mine[RANK_EACH];
     int before[RANK_EACH] = {};
 #pragma unroll
-    for (int u = 0; u < RANK_EACH; ++u) mine[u] = t0 + u < nnz ? key_of(t0 + u) : 0u;
-    if (t0 >= nnz) return;
-    for (int t = lane; t < nnz; t += 32) {
-        const uint32_t k = key_of(t);
+    for (int u = 0; u < RANK_EACH; ++u) mine[u] = keys[t0 + u];
+    for (int t = lane * 4; t < up; t += 128) {
+        const uint4 k = *reinterpret_cast<const uint4*>(keys + t);
 #pragma unroll
-        for (int u = 0; u < RANK_EACH; ++u) before[u] += k < mine[u] || (k == mine[u] && t < t0 + u);
+        for (int u = 0; u < RANK_EACH; ++u) {
+            // an entry before counts if its key is not larger, one behind if it is smaller; the entry itself does not
+            const int at = t0 + u - t;
+            before[u] += (at > 0 ? k.x <= mine[u] : k.x < mine[u]) + (at > 1 ? k.y <= mine[u] : k.y < mine[u]) + (at > 2 ? k.z <= mine[u] : k.z < mine[u]) +
+                         (at > 3 ? k.w <= mine[u] : k.w < mine[u]);
+        }
     }
 #pragma unroll
     for (int u = 0; u < RANK_EACH; ++u) {
         const int at = __reduce_add_sync(FULL_MASK, before[u]);
-        const int t = t0 + u;
-        if (lane != 0 || t >= nnz) continue;
+        if (lane != u || t0 + u >= nnz) continue;
         key[at] = mine[u];
-        row[at] = (uint32_t)a.row_of(t, 0, a.m - 1);
-        if (weight) weight[at] = weights[t];
-        if (mine[u] < (uint32_t)n) atomicOr(present + (mine[u] >> 5), 1u << (mine[u] & 31));
+        row[at] = (uint32_t)my_row;
+        if (weight) weight[at] = weights[t0 + u];
     }
 }
 
@@ -163,43 +259,36 @@ __device__ __forceinline__ void write_row(G* __restrict__ at, int64_t left, A sc
     store_narrow<G, V>(at, left, x);
 }
 
-// CTAs below `piece_ctas` add up pieces; those behind fill the rows of dE without entries, `fill_rows` each.
+// A group of lanes per piece and slab of columns.
+#ifndef PIECE_UNROLL
+#define PIECE_UNROLL 4
+#endif
+#ifndef PIECE_CTAS
+#define PIECE_CTAS 4
+#endif
 template <typename T, typename G, int V>
-__global__ void __launch_bounds__(THREADS) add_pieces_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
+__global__ void __launch_bounds__(THREADS, PIECE_CTAS) add_pieces_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
                                                              const uint32_t* __restrict__ row, const typename Wide<T>::type* __restrict__ weight,
                                                              typename Wide<T>::type scale, const T* __restrict__ dy, int64_t lddy, G* __restrict__ de,
                                                              int64_t ldde, bool accumulate, typename Wide<T>::type* __restrict__ part, int piece,
-                                                             int shift, int64_t slabs, int64_t piece_ctas, const uint32_t* __restrict__ present,
-                                                             int64_t fill_rows) {
+                                                             int shift, int64_t slabs) {
     using A = typename Wide<T>::type;
-    link(key, row, weight, present);
-    if ((int64_t)blockIdx.x >= piece_ctas) {
-        const int64_t v0 = ((int64_t)blockIdx.x - piece_ctas) * fill_rows, v1 = min(v0 + fill_rows, n);
-        // up to a warp per row: elements up to the first 16-byte boundary, 16 bytes a lane, the elements behind
-        const int fs = min(5, 32 - __clz((int)min((p * (int64_t)sizeof(G) + 15) / 16, (int64_t)32) - 1));
-        const int lane = threadIdx.x & ((1 << fs) - 1);
-        for (int64_t v = v0 + (threadIdx.x >> fs); v < v1; v += THREADS >> fs) {
-            if (present[v >> 5] >> (v & 31) & 1u) continue;
-            G* const at = de + v * ldde;
-            const int64_t head = min(p, (int64_t)((0 - reinterpret_cast<uintptr_t>(at)) % 16 / sizeof(G)));
-            const int64_t body = (p - head) / (16 / (int)sizeof(G)), tail = head + body * (16 / (int)sizeof(G));
-            for (int64_t c = lane; c < head; c += 1 << fs) at[c] = narrow<G>(typename Wide<G>::type(0));
-            for (int64_t c = lane; c < body; c += 1 << fs) reinterpret_cast<uint4*>(at + head)[c] = uint4{0, 0, 0, 0};
-            for (int64_t c = tail + lane; c < p; c += 1 << fs) at[c] = narrow<G>(typename Wide<G>::type(0));
-        }
-        return;
-    }
+    constexpr int U = PIECE_UNROLL;
+    link(key, row, weight);
     const int lane = threadIdx.x & ((1 << shift) - 1);
     const int64_t item = (int64_t)blockIdx.x * (THREADS >> shift) + (threadIdx.x >> shift);
     const int64_t at_piece = item / slabs, c = ((item - at_piece * slabs) << shift) * V + (int64_t)lane * V;
     const int64_t e0 = at_piece * piece, e1 = min(e0 + piece, nnz);
-    if (e0 >= nnz || c >= p) return;
+    if (e0 >= nnz) return;  // (the whole group)
+    // the lanes of a group that share a warp fetch an entry each and hand them round
+    const int share = 1 << min(shift, 5), in_share = threadIdx.x & (share - 1);
+    const unsigned mask = share == 32 ? FULL_MASK : ((1u << share) - 1) << (lane_id() & ~(share - 1));
     const uint32_t before = e0 > 0 ? key[e0 - 1] : NO_KEY, behind = e1 < nnz ? key[e1] : NO_KEY;
     A acc[V] = {};
     uint32_t cur = key[e0];
     bool open = cur == before;  // the run comes from the piece before
     auto finish = [&](bool goes_on) {
-        if (cur < (uint32_t)n) {
+        if (cur < (uint32_t)n && c < p) {
             if (!open && !goes_on) {
                 write_row<G, A, V>(de + (int64_t)cur * ldde + c, p - c, scale, accumulate, acc);
             } else {
@@ -212,146 +301,163 @@ __global__ void __launch_bounds__(THREADS) add_pieces_kernel(int64_t nnz, int64_
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = A(0);
     };
-    constexpr int U = 4;
-    for (int64_t e = e0; e < e1; e += U) {
-        uint32_t k[U], r[U];
-        A w[U], x[U][V];
+    for (int64_t e = e0; e < e1; e += share) {
+        const bool on = e + in_share < e1;
+        const uint32_t my_key = on ? key[e + in_share] : NO_KEY, my_row = on ? row[e + in_share] : 0u;
+        const A my_w = on && weight ? weight[e + in_share] : A(1);
+        const int count = (int)min((int64_t)share, e1 - e);
+        for (int q = 0; q < count; q += U) {
+            uint32_t k[U];
+            Vec<T, V> x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool on = e + u < e1;
-            k[u] = on ? key[e + u] : 0u;
-            r[u] = on ? row[e + u] : NO_KEY;
-            w[u] = on && weight ? weight[e + u] : A(1);
-            if (!on || k[u] >= (uint32_t)n) r[u] = NO_KEY;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_wide<T, V>(r[u] != NO_KEY ? dy + (int64_t)r[u] * lddy + c : dy, r[u] != NO_KEY ? p - c : 0, x[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (e + u >= e1) break;
-            if (k[u] != cur) {
-                finish(false);
-                cur = k[u];
-                open = false;
+            for (int u = 0; u < U; ++u) {
+                const uint32_t got = __shfl_sync(mask, my_key, q + u, share), r = __shfl_sync(mask, my_row, q + u, share);
+                k[u] = q + u < count ? got : NO_KEY;
+                if (k[u] < (uint32_t)n) x[u] = load_raw<T, V>(dy + (int64_t)r * lddy + c, p - c);
             }
-            if (r[u] != NO_KEY) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += w[u] * x[u][i];
+            for (int u = 0; u < U; ++u) {
+                const A w = weight ? __shfl_sync(mask, my_w, q + u, share) : A(1);
+                if (q + u >= count) continue;
+                if (k[u] != cur) {
+                    finish(false);
+                    cur = k[u];
+                    open = false;
+                }
+                if (k[u] < (uint32_t)n) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] += w * widen(x[u].x[i]);
+                }
             }
         }
     }
     finish(cur == behind);
 }
 
-// first entry behind those of id k (the keys ascend)
-__device__ __forceinline__ int64_t upper_bound(const uint32_t* __restrict__ key, int64_t lo, int64_t hi, uint32_t k) {
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] <= k) lo = mid + 1; else hi = mid;
-    }
-    return lo;
-}
-
-// The runs that cross pieces: a warp looks at eight pieces for runs that begin there and go on, and adds up the partial sums of a run
-// of up to JOIN_SHORT pieces by itself, JOIN_COLS columns per blockIdx.y.  The CTA takes the longer ones, every warp a
-// contiguous share of the pieces.
-constexpr int JOIN_COLS = 128;
-constexpr int JOIN_SHORT = 16;
-constexpr int JOIN_WARPS = THREADS / 32;
+// Joins the partial sums of JOIN pieces (of `piece` entries; blocks of pieces on the later levels): a CTA per block of pieces and
+// JOIN_COLS columns.  Every warp joins JOIN_EACH consecutive pieces, and the first warp then what the warps have left, in the same
+// way.  What ends inside is written to dE; what crosses the ends is a partial sum of the warp's pieces, of the block.  (A warp that walks all 64
+// pieces by itself takes 25 us, most of it waiting for its own instructions.)
+constexpr int JOIN_COLS = 64;
 constexpr int JOIN_EACH = 8;
-constexpr int JOIN_PIECES = JOIN_WARPS * JOIN_EACH;  // per CTA
-template <typename T, typename G>
-__global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
-                                                       const typename Wide<T>::type* __restrict__ part, typename Wide<T>::type scale,
-                                                       G* __restrict__ de, int64_t ldde, bool accumulate, int piece) {
-    using A = typename Wide<T>::type;
-    constexpr int EACH = JOIN_COLS / 32;  // columns of a lane
-    __shared__ A sums[JOIN_WARPS][JOIN_COLS];
-    __shared__ int64_t long_first[JOIN_PIECES], long_count[JOIN_PIECES];
-    __shared__ int long_runs;
+static_assert(JOIN == JOIN_EACH * (THREADS / 32), "a warp per JOIN_EACH pieces");
+
+// What joining has to know of JOIN_EACH consecutive pieces from `first` on: a bit each whether its first run comes from before, whether its last
+// one goes on, whether it is all one run; and, in lane q, the id of piece q's first entry.
+struct Seams {
+    unsigned open, on, one;
+    uint32_t id;
+    __device__ __forceinline__ Seams(const uint32_t* __restrict__ key, int64_t first, int64_t piece, int64_t nnz, int64_t n) {
+        const int64_t e0 = (first + lane_id()) * piece, e1 = min(e0 + piece, nnz);
+        bool is_open = false, is_on = false, is_one = false;
+        id = NO_KEY;
+        if (lane_id() < JOIN_EACH && e0 < nnz) {
+            id = key[e0];
+            const uint32_t last = key[e1 - 1], before = e0 > 0 ? key[e0 - 1] : NO_KEY, behind = e1 < nnz ? key[e1] : NO_KEY;
+            is_open = id < (uint32_t)n && before == id;
+            is_on = last < (uint32_t)n && behind == last;
+            is_one = id == last;
+        }
+        open = __ballot_sync(FULL_MASK, is_open);
+        on = __ballot_sync(FULL_MASK, is_on);
+        one = __ballot_sync(FULL_MASK, is_one);
+    }
+    // get(q, slot, x): the partial sums of piece q (slot 0: of the run from before, 1: of the one that begins there and goes on);
+    // write(id, x): a finished sum; leave(slot, x): a partial sum of all these pieces together
+    template <typename A, int N, typename Get, typename Write, typename Leave>
+    __device__ __forceinline__ void walk(Get get, Write write, Leave leave) const {
+        const unsigned begins = on & ~(open & one);  // a run begins in the piece and goes on
+        if ((open | begins) == 0) return;
+        A x[JOIN_EACH][2][N];
+#pragma unroll
+        for (int q = 0; q < JOIN_EACH; ++q) {
+            if (open >> q & 1) get(q, 0, x[q][0]);
+            if (begins >> q & 1) get(q, 1, x[q][1]);
+        }
+        A acc[N] = {};
+        bool from_before = open & 1;
+#pragma unroll
+        for (int q = 0; q < JOIN_EACH; ++q) {
+            if (open >> q & 1) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] += x[q][0][i];
+                if (!(one & on & 1u << q)) {  // ends here
+                    if (from_before) leave(0, acc);
+                    else write(__shfl_sync(FULL_MASK, id, q), acc);
+                    from_before = false;
+                }
+            }
+            if (begins >> q & 1) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] = x[q][1][i];
+            }
+        }
+        if (on >> (JOIN_EACH - 1) & 1) leave(from_before ? 0 : 1, acc);
+    }
+};
+
+template <typename A, typename G>
+__global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key, const A* __restrict__ part,
+                                                       A* __restrict__ part_out, A scale, G* __restrict__ de, int64_t ldde, bool accumulate, int64_t piece) {
+    constexpr int N = JOIN_COLS / 32;
+    __shared__ A left[THREADS / 32][2][JOIN_COLS];
     link(key, part);
     const int lane = lane_id(), warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) long_runs = 0;
-    __syncthreads();
-    // pieces that a run begins in and leaves; how many pieces it has
-    const int64_t f = (int64_t)blockIdx.x * JOIN_PIECES + warp * JOIN_EACH + lane;
-    int64_t count = 0;
-    if (lane < JOIN_EACH) {
-        const int64_t e0 = f * piece, e1 = min(e0 + piece, nnz);
-        if (e1 < nnz) {
-            const uint32_t k = key[e1 - 1];
-            if (k < (uint32_t)n && key[e1] == k && !(key[e0] == k && e0 > 0 && key[e0 - 1] == k)) count = (upper_bound(key, e1, nnz, k) - 1) / piece - f + 1;
-        }
-    }
-    if (count > JOIN_SHORT) {
-        const int at = atomicAdd(&long_runs, 1);  // (the order of the runs does not matter)
-        long_first[at] = f;
-        long_count[at] = count;
-    }
-    const int64_t c0 = (int64_t)blockIdx.y * JOIN_COLS + lane;
-    auto add = [&](int64_t first, int64_t s0, int64_t s1, A(&acc)[EACH]) {
-#pragma unroll 4
-        for (int64_t s = s0; s < s1; ++s) {
+    const int64_t c = (int64_t)blockIdx.y * JOIN_COLS + lane, first = (int64_t)blockIdx.x * JOIN + warp * JOIN_EACH;
+    auto write = [&](uint32_t id, A(&x)[N]) {
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (c0 + i * 32 < p) acc[i] += part[((first + s) * 2 + (s == 0 ? 1 : 0)) * p + c0 + i * 32];
+        for (int i = 0; i < N; ++i) {
+            A one[1] = {x[i]};
+            if (c + i * 32 < p) write_row<G, A, 1>(de + (int64_t)id * ldde + c + i * 32, 1, scale, accumulate, one);
         }
     };
-    auto write = [&](int64_t first, A(&acc)[EACH]) {
-        G* const at = de + (int64_t)key[first * piece + piece - 1] * ldde + c0;
+    const Seams mine(key, first, piece, nnz, n);
+    mine.walk<A, N>(
+        [&](int q, int slot, A(&x)[N]) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            A x[1] = {acc[i]};
-            if (c0 + i * 32 < p) write_row<G, A, 1>(at + i * 32, 1, scale, accumulate, x);
-        }
-    };
-    for (unsigned runs = __ballot_sync(FULL_MASK, count > 0 && count <= JOIN_SHORT); runs; runs &= runs - 1) {
-        const int from = __ffs(runs) - 1;
-        const int64_t first = __shfl_sync(FULL_MASK, f, from), pieces = __shfl_sync(FULL_MASK, count, from);
-        A acc[EACH] = {};
-        add(first, 0, pieces, acc);
-        write(first, acc);
-    }
+            for (int i = 0; i < N; ++i) x[i] = c + i * 32 < p ? part[((first + q) * 2 + slot) * p + c + i * 32] : A(0);
+        },
+        write,
+        [&](int slot, A(&x)[N]) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) left[warp][slot][i * 32 + lane] = x[i];
+        });
     __syncthreads();
-    for (int r = 0; r < long_runs; ++r) {
-        const int64_t first = long_first[r], pieces = long_count[r], share = (pieces + JOIN_WARPS - 1) / JOIN_WARPS;
-        A acc[EACH] = {};
-        add(first, min(pieces, warp * share), min(pieces, (warp + 1) * share), acc);
+    if (warp > 0) return;
+    const Seams all(key, (int64_t)blockIdx.x * (THREADS / 32), piece * JOIN_EACH, nnz, n);
+    all.walk<A, N>(
+        [&](int q, int slot, A(&x)[N]) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) sums[warp][lane + i * 32] = acc[i];
-        __syncthreads();
-        if (warp == 0) {
-            for (int w = 1; w < JOIN_WARPS; ++w) {
+            for (int i = 0; i < N; ++i) x[i] = left[q][slot][i * 32 + lane];
+        },
+        write,
+        [&](int slot, A(&x)[N]) {
 #pragma unroll
-                for (int i = 0; i < EACH; ++i) acc[i] += sums[w][lane + i * 32];
-            }
-            write(first, acc);
-        }
-        __syncthreads();
-    }
+            for (int i = 0; i < N; ++i)
+                if (c + i * 32 < p) part_out[((int64_t)blockIdx.x * 2 + slot) * p + c + i * 32] = x[i];
+        });
 }
 
 template <typename T, typename G, int V>
 spsyrk_status_t add_typed(const GradWs& w, int which, int64_t n, int64_t p, int64_t nnz, bool weighted, double scale, const void* dy, int64_t lddy, void* de,
                           int64_t ldde, bool accumulate, cudaStream_t st) {
     using A = typename Wide<T>::type;
-    const int piece = piece_of(nnz, p);
-    const int64_t pieces = (nnz + piece - 1) / piece, vectors = (p + V - 1) / V;
+    int64_t piece = piece_of(nnz, p);
+    int64_t pieces = (nnz + piece - 1) / piece;
+    const int64_t vectors = (p + V - 1) / V;
     int shift = 0;
     while ((int64_t(1) << shift) < vectors && shift < 8) ++shift;
     const int64_t slabs = (vectors + (int64_t(1) << shift) - 1) >> shift, per_cta = THREADS >> shift;
-    const int64_t piece_ctas = (pieces * slabs + per_cta - 1) / per_cta;
-    // about 64 KB of dE a CTA
-    const int64_t fill_rows = std::max<int64_t>(1, std::min<int64_t>(65536, 65536 / std::max<int64_t>(1, p * (int64_t)sizeof(G))));
-    const int64_t fill_ctas = accumulate ? 0 : (n + fill_rows - 1) / fill_rows;
-    if (piece_ctas + fill_ctas >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
+    const int64_t ctas = (pieces * slabs + per_cta - 1) / per_cta;
+    if (ctas >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
+    const uint32_t* const key = w.key[which];
     const A* weight = weighted ? static_cast<const A*>(w.weight[which]) : nullptr;
-    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)(piece_ctas + fill_ctas), THREADS, 0, st, nnz, n, p, w.key[which], w.row[which], weight,
-                                  (A)scale, static_cast<const T*>(dy), lddy, static_cast<G*>(de), ldde, accumulate, static_cast<A*>(w.part), piece, shift,
-                                  slabs, piece_ctas, w.present, fill_rows));
-    if (pieces > 1) {
+    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)ctas, THREADS, 0, st, nnz, n, p, key, w.row[which], weight, (A)scale,
+                                  static_cast<const T*>(dy), lddy, static_cast<G*>(de), ldde, accumulate, static_cast<A*>(w.part[0]), (int)piece, shift, slabs));
+    for (int level = 0; pieces > 1; ++level) {
+        const int64_t blocks = (pieces + JOIN - 1) / JOIN;
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)((pieces + JOIN_PIECES - 1) / JOIN_PIECES), (unsigned)((p + JOIN_COLS - 1) / JOIN_COLS));
+        cfg.gridDim = dim3((unsigned)blocks, (unsigned)((p + JOIN_COLS - 1) / JOIN_COLS));
         cfg.blockDim = dim3(THREADS);
         cfg.stream = st;
         cudaLaunchAttribute attr{};
@@ -359,28 +465,34 @@ spsyrk_status_t add_typed(const GradWs& w, int which, int64_t n, int64_t p, int6
         attr.val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        SPSYRK_CUDA_TRY(launch_kernel(cfg, join_kernel<T, G>, nnz, n, p, (const uint32_t*)w.key[which], static_cast<const A*>(w.part), (A)scale,
-                                      static_cast<G*>(de), ldde, accumulate, piece));
+        A* const out = level + 1 < JOIN_LEVELS ? static_cast<A*>(w.part[level + 1]) : nullptr;  // (null where one block holds all: nothing leaves it)
+        SPSYRK_CUDA_TRY(launch_kernel(cfg, join_kernel<A, G>, nnz, n, p, key, static_cast<const A*>(w.part[level]), out, (A)scale, static_cast<G*>(de), ldde,
+                                      accumulate, piece));
+        piece *= JOIN;
+        pieces = blocks;
     }
     return SPSYRK_OK;
 }
 
-// Orders the entries; *which receives the buffer that they are in.
+// Orders the entries and fills the rows without any (fill.rows == 0: leaves them); *which receives the buffer that the entries are in.
 template <typename A>
-spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const int32_t* ids, const void* weights, int* which, cudaStream_t st) {
-    SPSYRK_CUDA_TRY(cudaMemsetAsync(w.zero, 0, w.zero_bytes, st));
+spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const int32_t* ids, const void* weights, Fill fill, int* which, cudaStream_t st) {
     const A* wv = static_cast<const A*>(weights);
     if (a.nnz <= FEW) {
-        const int64_t each = THREADS / 32 * RANK_EACH;
-        rank_kernel<A><<<(unsigned)((a.nnz + each - 1) / each), THREADS, 0, st>>>(a, n, ids, wv, w.key[0], w.row[0], static_cast<A*>(weights ? w.weight[0] : nullptr),
-                                                                              w.present);
+        const int64_t ctas = (a.nnz + RANK_HERE - 1) / RANK_HERE;
+        // (a CTA that fills looks all ids through: few, then)
+        if (fill.rows) fill.rows = std::min<int64_t>(FILL_MOST, std::max<int64_t>(fill.rows, (n + SMS * 4 - 1) / (SMS * 4)));
+        const int64_t fill_ctas = fill.rows ? (n + fill.rows - 1) / fill.rows : 0;
+        rank_kernel<A><<<(unsigned)(ctas + fill_ctas), THREADS, 0, st>>>(a, n, ids, wv, w.key[0], w.row[0], static_cast<A*>(weights ? w.weight[0] : nullptr), (int)ctas,
+                                                                         fill);
         note_launches(1);
         SPSYRK_CUDA_TRY(cudaGetLastError());
         *which = 0;
         return SPSYRK_OK;
     }
+    SPSYRK_CUDA_TRY(cudaMemsetAsync(w.zero, 0, w.zero_bytes, st));
     const int passes = radix_passes((uint64_t)n);
-    read_ids_kernel<<<(unsigned)((a.nnz + READ_CHUNK - 1) / READ_CHUNK), THREADS, 0, st>>>(a, n, ids, w.key[0], w.row[0], w.present, passes, w.rs.bins);
+    read_ids_kernel<<<(unsigned)std::min<int64_t>((a.nnz + READ_CHUNK - 1) / READ_CHUNK, SMS * 4), THREADS, 0, st>>>(a, n, ids, w.key[0], w.row[0], w.present, passes, w.rs.bins);
     note_launches(1);
     SPSYRK_CUDA_TRY(cudaGetLastError());
     using PB = typename std::conditional<sizeof(A) == 8, uint64_t, uint32_t>::type;
@@ -388,7 +500,12 @@ spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const i
         const int from = q & 1, to = from ^ 1;
         const PB* pb = weights ? reinterpret_cast<const PB*>(q == 0 ? weights : w.weight[from]) : nullptr;
         EmitOrdered<PB> emit{w.key[to], w.row[to], weights ? static_cast<PB*>(w.weight[to]) : nullptr};
-        SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st)));
+        if (fill.rows) {
+            const FillWithPass along{fill, w.present, n * q / passes, n * (q + 1) / passes};
+            SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st, along)));
+        } else {
+            SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st)));
+        }
     }
     *which = passes & 1;
     return SPSYRK_OK;
@@ -403,7 +520,7 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     if (!workspace_bytes || m < 0 || n < 0 || p < 0 || nnz < 0 || !is_real(dtype)) return SPSYRK_ERR_INVALID_ARG;
     if (g_dtype != dtype && !(g_dtype == SPSYRK_F32 && dtype != SPSYRK_F64)) return SPSYRK_ERR_INVALID_ARG;
     constexpr int64_t most = (int64_t(1) << 31) - 1;
-    if (m >= most || n >= most || nnz >= most || p > (int64_t(1) << 22)) return SPSYRK_ERR_OVERFLOW;
+    if (m >= most || n >= most || nnz >= most || p > (int64_t(1) << 21)) return SPSYRK_ERR_OVERFLOW;
     // (the size with room for weights: a query need not know whether there are any)
     const size_t need = carve(nullptr, nullptr, n, p, nnz, dtype == SPSYRK_F64, true);
     if (!d_workspace) {
@@ -425,9 +542,12 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     const Rows a{d_rowptr, m, nnz, nnz / m};
     GradWs w;
     carve(&w, d_workspace, n, p, nnz, dtype == SPSYRK_F64, true);
+    // 256 KB of dE a CTA, at most 512 rows
+    const int64_t used = p * (int64_t)g_size;
+    const Fill fill{static_cast<char*>(d_de), ldde * (int64_t)g_size, used, (int)g_size, accumulate ? 0 : std::max<int64_t>(1, std::min<int64_t>(512, (1 << 18) / used)), n};
     int which = 0;
-    const spsyrk_status_t s = dtype == SPSYRK_F64 ? order_entries<double>(w, a, n, d_ids, d_weights, &which, st)
-                                                  : order_entries<float>(w, a, n, d_ids, d_weights, &which, st);
+    const spsyrk_status_t s = dtype == SPSYRK_F64 ? order_entries<double>(w, a, n, d_ids, d_weights, fill, &which, st)
+                                                  : order_entries<float>(w, a, n, d_ids, d_weights, fill, &which, st);
     if (s != SPSYRK_OK) return s;
     const bool wide = aligned16(d_dy, lddy, size) && aligned16(d_de, ldde, g_size);
     const bool weighted = d_weights != nullptr;

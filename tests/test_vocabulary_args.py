@@ -61,7 +61,7 @@ def test_lookups_refuse(lib, call):
     for changes in (dict(m=-1, nnz=0), dict(n=-1), dict(p=-1), dict(nnz=-1), dict(dtype=Code(I32)), dict(dtype=Code(5)), dict(dtype=Code(-1)), dict(lde=7),
                     {other: 7}, dict(ids=None), dict(e=None), {"y" if call is lookup else "dw": None}, dict(nnz=7), dict(m=0)):
         assert call(lib, **changes) == INVALID, changes
-    for changes in (dict(m=MOST, nnz=0), dict(n=MOST), dict(nnz=MOST), dict(p=(1 << 22) + 1, lde=1 << 23, **{other: 1 << 23})):
+    for changes in (dict(m=MOST, nnz=0), dict(n=MOST), dict(nnz=MOST), dict(p=(1 << 21) + 1, lde=1 << 23, **{other: 1 << 23})):
         assert call(lib, **changes) == OVERFLOW, changes
     if call is lookup:
         assert call(lib, m=0, nnz=0) == 0 and call(lib, p=0) == 0
@@ -76,7 +76,7 @@ def test_lookup_grad_refuses(lib):
     for changes in (dict(m=-1), dict(n=-1), dict(p=-1), dict(nnz=-1), dict(dtype=Code(I32)), dict(gdtype=Code(BF16)), dict(gdtype=Code(F64)),
                     dict(dtype=Code(F64)), dict(dtype=Code(BF16), gdtype=Code(F16))):
         assert lookup_grad(lib, **changes)[0] == INVALID, changes
-    for changes in (dict(m=MOST), dict(n=MOST), dict(nnz=MOST), dict(p=(1 << 22) + 1)):
+    for changes in (dict(m=MOST), dict(n=MOST), dict(nnz=MOST), dict(p=(1 << 21) + 1)):
         assert lookup_grad(lib, **changes)[0] == OVERFLOW, changes
     assert lookup_grad(lib, AT, size - 1)[0] == WORKSPACE
     assert lookup_grad(lib, ctypes.c_void_p(4097), size)[0] == INVALID
