@@ -5,8 +5,8 @@
 // inside the piece is written to its row of dE at once, one that crosses the piece's ends leaves its partial sum in the workspace.  The
 // partial sums of such runs are joined in their order, 64 pieces at a time, then 64 times 64, until one block holds them all.  No atomic
 // adds: the same call gives the same bits, and an id that every tenth entry has costs no more than others (joined by one CTA
-// its 5500 pieces of 64 columns took 270 us).  Rows of ids that do not occur are filled with zeros by CTAs that go along with the sort,
-// which leaves the memory idle.
+// its 5500 pieces of 64 columns took 270 us).  Rows of ids that do not occur are filled with zeros by CTAs that stand among those that
+// add up pieces (or rank the ids, if they are few).
 // Bound by memory: dY is read once (a row of several ids once per id, through L2), dE written once.
 #include <algorithm>
 
@@ -37,7 +37,7 @@ constexpr int JOIN_LEVELS = 6;  // 2^31 entries in pieces of MIN_PIECE: 2^29, 2^
 struct GradWs {
     uint32_t *key[2], *row[2];  // ids (n: padding) and rows of the entries, before and after a pass
     void* weight[2];
-    uint32_t* present;  // a bit per id
+    uint8_t* present;  // a byte per id: it occurs
     // [pieces][2][p] partial sums: of a run that comes from the piece before, of one that begins here and goes on; then those of blocks of
     // JOIN pieces, of JOIN times JOIN, down to a single one
     void* part[JOIN_LEVELS];
@@ -70,14 +70,14 @@ size_t carve(GradWs* w, void* ws, int64_t n, int64_t p, int64_t nnz, bool wide, 
         count = (count + JOIN - 1) / JOIN;
     }
     // what has to be zero at the start, in one piece
-    const size_t bits = ((size_t)n / 32 + 1) * 4 / 8 * 8 + 8;
+    const size_t marks = nnz > FEW ? ((size_t)n + 7) / 8 * 8 : 0;
     const size_t words = nnz > FEW ? radix_state_words(radix_tiles(nnz), radix_wide(nnz), radix_passes((uint64_t)n)) : 0;
-    t.zero_bytes = bits + (1 + RX_MAX_PASSES * RX_BINS + RX_MAX_PASSES + words) * 8;
+    t.zero_bytes = marks + (1 + RX_MAX_PASSES * RX_BINS + RX_MAX_PASSES + words) * 8;
     t.zero = take(t.zero_bytes);
     char* z = (char*)t.zero;
-    t.present = (uint32_t*)z;
-    t.err = (uint32_t*)(z + bits);
-    t.rs.bins = (unsigned long long*)(z + bits) + 1;
+    t.present = (uint8_t*)z;
+    t.err = (uint32_t*)(z + marks);
+    t.rs.bins = (unsigned long long*)(z + marks) + 1;
     t.rs.tickets = (uint32_t*)(t.rs.bins + RX_MAX_PASSES * RX_BINS);
     t.rs.words = t.rs.bins + RX_MAX_PASSES * RX_BINS + RX_MAX_PASSES;
     if (w) *w = t;
@@ -120,14 +120,16 @@ struct Fill {
     }
 };
 
-// Key and row of every entry, a bit per id that occurs and the sizes of all digits.
+// Key and row of every entry, a mark per id that occurs and the sizes of all digits.
 constexpr int READ_ITEMS = 4;
 constexpr int READ_CHUNK = THREADS * READ_ITEMS;  // a step of a CTA
+constexpr int READ_LOG_MARKS = 11, READ_MARKS = 1 << READ_LOG_MARKS;
 __global__ void __launch_bounds__(THREADS) read_ids_kernel(Rows a, int64_t n, const int32_t* __restrict__ ids, uint32_t* __restrict__ key,
-                                                           uint32_t* __restrict__ row, uint32_t* present, int passes,
+                                                           uint32_t* __restrict__ row, uint8_t* __restrict__ present, int passes,
                                                            unsigned long long* __restrict__ bins) {
     __shared__ int64_t span[2];
     __shared__ uint32_t h[RX_MAX_PASSES][RX_BINS];
+    __shared__ uint64_t marks[READ_MARKS];
     for (int d = threadIdx.x; d < RX_MAX_PASSES * RX_BINS; d += THREADS) (&h[0][0])[d] = 0;
     for (int64_t base = (int64_t)blockIdx.x * READ_CHUNK; base < a.nnz; base += (int64_t)gridDim.x * READ_CHUNK) {
         __syncthreads();
@@ -137,22 +139,28 @@ __global__ void __launch_bounds__(THREADS) read_ids_kernel(Rows a, int64_t n, co
         }
         __syncthreads();
         uint32_t k[READ_ITEMS];
-        uint32_t seen[READ_ITEMS];
 #pragma unroll
         for (int i = 0; i < READ_ITEMS; ++i) {
             const int64_t t = base + i * THREADS + threadIdx.x, id = t < a.nnz ? ids[t] : -1;
             k[i] = id >= 0 && id < n && a.covered(t) ? (uint32_t)id : (uint32_t)n;
         }
-        // (looked at first: an id that every tenth of 2 million entries has took 100 us of atomic operations on one word)
+        // An id is marked by one of the CTA's entries that have it: an id's slot holds one of those whose ids share it.  (Atomic operations
+        // on a bit per id, a tenth of 2 million on the same one, took 55 us more, and 25 with this look.)
+        auto mark_of = [&](uint32_t id) { return (int)((id * 2654435761u) >> (32 - READ_LOG_MARKS)); };
 #pragma unroll
-        for (int i = 0; i < READ_ITEMS; ++i) seen[i] = __ldcg(present + (k[i] >> 5));
+        for (int i = 0; i < READ_ITEMS; ++i) {
+            marks[mark_of(k[i])] = (uint64_t)k[i] << 32 | (uint32_t)(i * THREADS + threadIdx.x);
+        }
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < READ_ITEMS; ++i) {
             const int64_t t = base + i * THREADS + threadIdx.x;
             if (t >= a.nnz) continue;
             key[t] = k[i];
             row[t] = (uint32_t)(a.rowptr ? a.row_of(t, span[0], span[1]) : t / a.k);
-            if (k[i] < (uint32_t)n && !(seen[i] >> (k[i] & 31) & 1u)) atomicOr(present + (k[i] >> 5), 1u << (k[i] & 31));
+            const uint64_t mark = marks[mark_of(k[i])];
+            const bool other = (uint32_t)(mark >> 32) == k[i] && (uint32_t)mark != (uint32_t)(i * THREADS + threadIdx.x);
+            if (k[i] < (uint32_t)n && !other) present[k[i]] = 1;
             for (int q = 0; q < passes; ++q) atomicAdd(&h[q][(k[i] >> (q * RX_BITS)) & (RX_BINS - 1)], 1u);
         }
     }
@@ -160,19 +168,6 @@ __global__ void __launch_bounds__(THREADS) read_ids_kernel(Rows a, int64_t n, co
     for (int d = threadIdx.x; d < passes * RX_BINS; d += THREADS)
         if ((&h[0][0])[d]) atomicAdd(&bins[d], (unsigned long long)(&h[0][0])[d]);
 }
-
-// A share of the rows, as work that goes along with a radix pass.
-struct FillWithPass {
-    static constexpr bool IS_SOME = true;
-    Fill fill;
-    const uint32_t* present;
-    int64_t begin, end;
-    unsigned ctas() const { return (unsigned)((end - begin + fill.rows - 1) / fill.rows); }
-    __device__ __forceinline__ void operator()(int64_t cta) const {
-        const int64_t v0 = begin + cta * fill.rows;
-        fill.rows_of(v0, min(v0 + fill.rows, end), [&](int64_t v) { return (__ldcg(present + (v >> 5)) >> (v & 31) & 1u) != 0; });
-    }
-};
 
 // Up to FEW entries: an entry's place in the order is the number of entries with a smaller id, or with the same one before it.  All
 // keys are fetched to shared memory, and a warp counts for four entries at a time, 128 keys a step.  CTAs behind those of the entries fill rows: they
@@ -260,23 +255,25 @@ __device__ __forceinline__ void write_row(G* __restrict__ at, int64_t left, A sc
 }
 
 // A group of lanes per piece and slab of columns.
-#ifndef PIECE_UNROLL
-#define PIECE_UNROLL 4
-#endif
-#ifndef PIECE_CTAS
-#define PIECE_CTAS 4
-#endif
+// (Registers decide: eight sums a lane take four rows at a time and three CTAs per SM, fewer sums two and five; the others cost 5 to 15 %.)
 template <typename T, typename G, int V>
-__global__ void __launch_bounds__(THREADS, PIECE_CTAS) add_pieces_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
+__global__ void __launch_bounds__(THREADS, V == 8 ? 3 : 5) add_pieces_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
                                                              const uint32_t* __restrict__ row, const typename Wide<T>::type* __restrict__ weight,
                                                              typename Wide<T>::type scale, const T* __restrict__ dy, int64_t lddy, G* __restrict__ de,
                                                              int64_t ldde, bool accumulate, typename Wide<T>::type* __restrict__ part, int piece,
-                                                             int shift, int64_t slabs) {
+                                                             int shift, int64_t slabs, const uint8_t* __restrict__ present, Fill fill, int fill_ctas) {
     using A = typename Wide<T>::type;
-    constexpr int U = PIECE_UNROLL;
-    link(key, row, weight);
+    constexpr int U = V == 8 ? 4 : 2;
+    link(key, row, weight, present);
+    // CTAs that fill rows stand evenly among the others
+    const int64_t filled = (int64_t)blockIdx.x * fill_ctas / gridDim.x;
+    if (((int64_t)blockIdx.x + 1) * fill_ctas / gridDim.x != filled) {
+        const int64_t v0 = filled * fill.rows;
+        fill.rows_of(v0, min(v0 + fill.rows, n), [&](int64_t v) { return present[v] != 0; });
+        return;
+    }
     const int lane = threadIdx.x & ((1 << shift) - 1);
-    const int64_t item = (int64_t)blockIdx.x * (THREADS >> shift) + (threadIdx.x >> shift);
+    const int64_t item = (blockIdx.x - filled) * (THREADS >> shift) + (threadIdx.x >> shift);
     const int64_t at_piece = item / slabs, c = ((item - at_piece * slabs) << shift) * V + (int64_t)lane * V;
     const int64_t e0 = at_piece * piece, e1 = min(e0 + piece, nnz);
     if (e0 >= nnz) return;  // (the whole group)
@@ -439,7 +436,7 @@ __global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, i
 }
 
 template <typename T, typename G, int V>
-spsyrk_status_t add_typed(const GradWs& w, int which, int64_t n, int64_t p, int64_t nnz, bool weighted, double scale, const void* dy, int64_t lddy, void* de,
+spsyrk_status_t add_typed(const GradWs& w, int which, const Fill& fill, int64_t n, int64_t p, int64_t nnz, bool weighted, double scale, const void* dy, int64_t lddy, void* de,
                           int64_t ldde, bool accumulate, cudaStream_t st) {
     using A = typename Wide<T>::type;
     int64_t piece = piece_of(nnz, p);
@@ -449,11 +446,13 @@ spsyrk_status_t add_typed(const GradWs& w, int which, int64_t n, int64_t p, int6
     while ((int64_t(1) << shift) < vectors && shift < 8) ++shift;
     const int64_t slabs = (vectors + (int64_t(1) << shift) - 1) >> shift, per_cta = THREADS >> shift;
     const int64_t ctas = (pieces * slabs + per_cta - 1) / per_cta;
-    if (ctas >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
+    const int64_t fill_ctas = fill.rows ? (n + fill.rows - 1) / fill.rows : 0;
+    if (ctas + fill_ctas >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
     const uint32_t* const key = w.key[which];
     const A* weight = weighted ? static_cast<const A*>(w.weight[which]) : nullptr;
-    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)ctas, THREADS, 0, st, nnz, n, p, key, w.row[which], weight, (A)scale,
-                                  static_cast<const T*>(dy), lddy, static_cast<G*>(de), ldde, accumulate, static_cast<A*>(w.part[0]), (int)piece, shift, slabs));
+    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)(ctas + fill_ctas), THREADS, 0, st, nnz, n, p, key, w.row[which], weight, (A)scale,
+                                  static_cast<const T*>(dy), lddy, static_cast<G*>(de), ldde, accumulate, static_cast<A*>(w.part[0]), (int)piece, shift, slabs, w.present, fill,
+                                  (int)fill_ctas));
     for (int level = 0; pieces > 1; ++level) {
         const int64_t blocks = (pieces + JOIN - 1) / JOIN;
         cudaLaunchConfig_t cfg{};
@@ -474,25 +473,27 @@ spsyrk_status_t add_typed(const GradWs& w, int which, int64_t n, int64_t p, int6
     return SPSYRK_OK;
 }
 
-// Orders the entries and fills the rows without any (fill.rows == 0: leaves them); *which receives the buffer that the entries are in.
+// Orders the entries; *which receives the buffer that they are in.  Few entries: also fills the rows without any, and sets fill->rows to 0.
 template <typename A>
-spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const int32_t* ids, const void* weights, Fill fill, int* which, cudaStream_t st) {
+spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const int32_t* ids, const void* weights, Fill* fill, int* which, cudaStream_t st) {
     const A* wv = static_cast<const A*>(weights);
     if (a.nnz <= FEW) {
         const int64_t ctas = (a.nnz + RANK_HERE - 1) / RANK_HERE;
         // (a CTA that fills looks all ids through: few, then)
-        if (fill.rows) fill.rows = std::min<int64_t>(FILL_MOST, std::max<int64_t>(fill.rows, (n + SMS * 4 - 1) / (SMS * 4)));
-        const int64_t fill_ctas = fill.rows ? (n + fill.rows - 1) / fill.rows : 0;
+        if (fill->rows) fill->rows = std::min<int64_t>(FILL_MOST, std::max<int64_t>(fill->rows, (n + SMS * 4 - 1) / (SMS * 4)));
+        const int64_t fill_ctas = fill->rows ? (n + fill->rows - 1) / fill->rows : 0;
         rank_kernel<A><<<(unsigned)(ctas + fill_ctas), THREADS, 0, st>>>(a, n, ids, wv, w.key[0], w.row[0], static_cast<A*>(weights ? w.weight[0] : nullptr), (int)ctas,
-                                                                         fill);
+                                                                         *fill);
         note_launches(1);
         SPSYRK_CUDA_TRY(cudaGetLastError());
+        fill->rows = 0;
         *which = 0;
         return SPSYRK_OK;
     }
     SPSYRK_CUDA_TRY(cudaMemsetAsync(w.zero, 0, w.zero_bytes, st));
     const int passes = radix_passes((uint64_t)n);
-    read_ids_kernel<<<(unsigned)std::min<int64_t>((a.nnz + READ_CHUNK - 1) / READ_CHUNK, SMS * 4), THREADS, 0, st>>>(a, n, ids, w.key[0], w.row[0], w.present, passes, w.rs.bins);
+    read_ids_kernel<<<(unsigned)std::min<int64_t>((a.nnz + READ_CHUNK - 1) / READ_CHUNK, SMS * 4), THREADS, 0, st>>>(a, n, ids, w.key[0], w.row[0], w.present, passes,
+                                                                                                               w.rs.bins);
     note_launches(1);
     SPSYRK_CUDA_TRY(cudaGetLastError());
     using PB = typename std::conditional<sizeof(A) == 8, uint64_t, uint32_t>::type;
@@ -500,12 +501,7 @@ spsyrk_status_t order_entries(const GradWs& w, const Rows& a, int64_t n, const i
         const int from = q & 1, to = from ^ 1;
         const PB* pb = weights ? reinterpret_cast<const PB*>(q == 0 ? weights : w.weight[from]) : nullptr;
         EmitOrdered<PB> emit{w.key[to], w.row[to], weights ? static_cast<PB*>(w.weight[to]) : nullptr};
-        if (fill.rows) {
-            const FillWithPass along{fill, w.present, n * q / passes, n * (q + 1) / passes};
-            SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st, along)));
-        } else {
-            SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st)));
-        }
+        SPSYRK_CUDA_TRY((radix_pass<PB, false>(w.key[from], w.row[from], pb, nullptr, a.nnz, q, w.rs, emit, w.err, st)));
     }
     *which = passes & 1;
     return SPSYRK_OK;
@@ -544,14 +540,14 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     carve(&w, d_workspace, n, p, nnz, dtype == SPSYRK_F64, true);
     // 256 KB of dE a CTA, at most 512 rows
     const int64_t used = p * (int64_t)g_size;
-    const Fill fill{static_cast<char*>(d_de), ldde * (int64_t)g_size, used, (int)g_size, accumulate ? 0 : std::max<int64_t>(1, std::min<int64_t>(512, (1 << 18) / used)), n};
+    Fill fill{static_cast<char*>(d_de), ldde * (int64_t)g_size, used, (int)g_size, accumulate ? 0 : std::max<int64_t>(1, std::min<int64_t>(512, (1 << 18) / used)), n};
     int which = 0;
-    const spsyrk_status_t s = dtype == SPSYRK_F64 ? order_entries<double>(w, a, n, d_ids, d_weights, fill, &which, st)
-                                                  : order_entries<float>(w, a, n, d_ids, d_weights, fill, &which, st);
+    const spsyrk_status_t s = dtype == SPSYRK_F64 ? order_entries<double>(w, a, n, d_ids, d_weights, &fill, &which, st)
+                                                  : order_entries<float>(w, a, n, d_ids, d_weights, &fill, &which, st);
     if (s != SPSYRK_OK) return s;
     const bool wide = aligned16(d_dy, lddy, size) && aligned16(d_de, ldde, g_size);
     const bool weighted = d_weights != nullptr;
-#define ADD(T, G, V) add_typed<T, G, V>(w, which, n, p, nnz, weighted, scale, d_dy, lddy, d_de, ldde, accumulate != 0, st)
+#define ADD(T, G, V) add_typed<T, G, V>(w, which, fill, n, p, nnz, weighted, scale, d_dy, lddy, d_de, ldde, accumulate != 0, st)
     switch (dtype) {
         case SPSYRK_F64: return wide ? ADD(double, double, 2) : ADD(double, double, 1);
         case SPSYRK_F32: return wide ? ADD(float, float, 4) : ADD(float, float, 1);

@@ -137,13 +137,6 @@ constexpr uint32_t NO_KEY = 0xffffffffu;
 template <typename Emit, typename = void> struct EmitNeighbours : std::false_type {};
 template <typename Emit> struct EmitNeighbours<Emit, std::void_t<decltype(Emit::NEIGHBOURS)>> : std::true_type {};
 
-// Work that goes along with a pass: CTAs behind those of the tiles call it with their number among them.
-struct NothingElse {
-    static constexpr bool IS_SOME = false;
-    unsigned ctas() const { return 0; }
-    __device__ __forceinline__ void operator()(int64_t) const {}
-};
-
 // `err` is the device error word of the caller: set by a look-back that gives up (and by the bounds-checked build).
 // Emit(dest, key, pa, pb) is called once per element with its position `dest` in the order sorted
 // by the digits seen so far.  pa == nullptr (pb == nullptr) means "this payload is the element's own
@@ -158,11 +151,11 @@ struct NothingElse {
 // An element whose position is not in [0, n) is dropped: it takes keys that were not counted (a matrix that failed its
 // checks, which the caller learns of later).  Then places of the output also stay unwritten, and what the next pass reads
 // there is whatever the memory held: an emit that indexes by a payload tests it.
-template <int BITS, typename PB, typename Emit, bool HAS_PC, typename S, typename Else = NothingElse>
+template <int BITS, typename PB, typename Emit, bool HAS_PC, typename S>
 __global__ void __launch_bounds__(RX_THREADS, 2) radix_scatter_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ pa,
                                                                       const PB* __restrict__ pb, const uint32_t* __restrict__ pc,
                                                                       int64_t n, int shift, const unsigned long long* __restrict__ bins,
-                                                                      S* __restrict__ words, uint32_t* __restrict__ ticket, Emit emit, uint32_t* err, Else also) {
+                                                                      S* __restrict__ words, uint32_t* __restrict__ ticket, Emit emit, uint32_t* err) {
     constexpr int NB = 1 << BITS;
     static_assert(BITS <= 12, "digit width");
     extern __shared__ __align__(16) unsigned char rx_smem[];
@@ -182,13 +175,6 @@ __global__ void __launch_bounds__(RX_THREADS, 2) radix_scatter_kernel(const uint
     // (What is read of the elements lies where the ticket says, which is drawn behind this; with their pointers handed to link
     // they were no loads of constants any more and registers were spilled: a pass over 1.7e7 nonzeros took 250 us instead of 240.)
     link();
-    if constexpr (Else::IS_SOME) {
-        const int64_t tiles = (n + RX_TILE - 1) / RX_TILE;
-        if ((int64_t)blockIdx.x >= tiles) {
-            also((int64_t)blockIdx.x - tiles);
-            return;
-        }
-    }
     if (tid == 0) s_tile = atomicAdd(ticket, 1u);
     __syncthreads();
     const int64_t tile = s_tile, tile_base = tile * RX_TILE;
@@ -314,23 +300,23 @@ struct EmitArrays3 {
 };
 
 // pass `pass` of a sort whose state has been set up (zeroed, bins counted)
-template <typename PB, bool HAS_PC, typename Emit, typename S, typename Else>
+template <typename PB, bool HAS_PC, typename Emit, typename S>
 inline cudaError_t radix_pass_launch(const uint32_t* keys, const uint32_t* pa, const PB* pb, const uint32_t* pc, int64_t n, int pass, const RadixState& rs,
-                                     Emit emit, uint32_t* err, cudaStream_t st, Else also) {
+                                     Emit emit, uint32_t* err, cudaStream_t st) {
     const int64_t nt = radix_tiles(n);
-    auto kern = radix_scatter_kernel<RX_BITS, PB, Emit, HAS_PC, S, Else>;
+    auto kern = radix_scatter_kernel<RX_BITS, PB, Emit, HAS_PC, S>;
     const size_t smem = RadixSmem<RX_BITS, PB, HAS_PC>::bytes();
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_linked(kern, (unsigned)nt + also.ctas(), RX_THREADS, smem, st, keys, pa, pb, pc, n, pass * RX_BITS, rs.bins + pass * RX_BINS,
-                         static_cast<S*>(rs.words) + (size_t)pass * nt * RX_BINS, rs.tickets + pass, emit, err, also);
+    return launch_linked(kern, (unsigned)nt, RX_THREADS, smem, st, keys, pa, pb, pc, n, pass * RX_BITS, rs.bins + pass * RX_BINS,
+                         static_cast<S*>(rs.words) + (size_t)pass * nt * RX_BINS, rs.tickets + pass, emit, err);
 }
-template <typename PB, bool HAS_PC, typename Emit, typename Else = NothingElse>
+template <typename PB, bool HAS_PC, typename Emit>
 inline cudaError_t radix_pass(const uint32_t* keys, const uint32_t* pa, const PB* pb, const uint32_t* pc, int64_t n, int pass, const RadixState& rs, Emit emit,
-                              uint32_t* err, cudaStream_t st, Else also = {}) {
+                              uint32_t* err, cudaStream_t st) {
     if (n <= 0) return cudaSuccess;
-    return radix_wide(n) ? radix_pass_launch<PB, HAS_PC, Emit, unsigned long long>(keys, pa, pb, pc, n, pass, rs, emit, err, st, also)
-                         : radix_pass_launch<PB, HAS_PC, Emit, uint32_t>(keys, pa, pb, pc, n, pass, rs, emit, err, st, also);
+    return radix_wide(n) ? radix_pass_launch<PB, HAS_PC, Emit, unsigned long long>(keys, pa, pb, pc, n, pass, rs, emit, err, st)
+                         : radix_pass_launch<PB, HAS_PC, Emit, uint32_t>(keys, pa, pb, pc, n, pass, rs, emit, err, st);
 }
 
 inline int bits_for(uint64_t max_value) {
