@@ -8,6 +8,7 @@ there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -536,24 +537,23 @@ def spsyrk_jaccard(m, row_begin, rows, a_rowptr, c_rowptr, c_colidx, c_counts, o
 # Rows of ids and dense matrices: lookups, their gradients, distillation.  The work goes to the tensors' device whatever the
 # current one is, to `stream` or to the current stream of that device.
 # ------------------------------------------------------------------------------------------
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (torch.cuda's functions take 7 us of a call's 15)
 
 
 def _call(fn, where, tensors, stream, *args):
     """fn(*args, stream) on the device of the tensors (None among them is skipped), which must be one."""
-    device = tensors[0].device
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device != device):
+        if t is not None and (t.get_device() != device or device < 0):
             raise ValueError(f"{where}: tensors must be CUDA tensors on one device")
-    if stream is not None and stream.device != device:
+    if stream is not None and stream.device.index != device:
         raise ValueError(f"{where}: the stream belongs to another device")
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    if device.index == torch.cuda.current_device():
-        status = fn(*args, s.cuda_stream)
+    at = _raw_stream(device) if stream is None else stream.cuda_stream
+    if device == _current_device():
+        status = fn(*args, at)
     else:
         with torch.cuda.device(device):
-            status = fn(*args, s.cuda_stream)
+            status = fn(*args, at)
     if status != OK:
         raise SpsyrkError(status, where)
 
@@ -562,15 +562,17 @@ def _matrix(t, where, name, rows=None, cols=None, dtype=None):
     """The row stride of a dense matrix whose rows are contiguous."""
     if t.dim() != 2 or t.dtype not in _REAL_CODE or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{where}: {name} must be a matrix of {dtype or 'float64, float32, bfloat16 or float16'}")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not ({rows}, {cols})")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    m, n = t.shape
+    if (rows is not None and m != rows) or (cols is not None and n != cols):
+        raise ValueError(f"{where}: {name} has shape ({m}, {n}), not ({rows}, {cols})")
+    ld, step = t.stride()
+    if n > 1 and step != 1:
         raise ValueError(f"{where}: the rows of {name} must be contiguous")
-    if t.shape[0] < 2:
-        return max(t.shape[1], 1)
-    if t.stride(0) < t.shape[1]:
+    if m < 2:
+        return max(n, 1)
+    if ld < n:
         raise ValueError(f"{where}: the rows of {name} overlap")
-    return t.stride(0)
+    return ld
 
 
 def _entries(where, ids, rowptr, values, dtypes, name):
@@ -590,6 +592,10 @@ def _entries(where, ids, rowptr, values, dtypes, name):
     return m, ids.numel()
 
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _weight_dtype(dtype):
     return torch.float64 if dtype == torch.float64 else torch.float32
 
@@ -601,7 +607,7 @@ def spsyrk_lookup(ids, e, rowptr=None, weights=None, scale=1.0, y=None, stream=N
     m, nnz = _entries("spsyrk_lookup", ids, rowptr, weights, (_weight_dtype(e.dtype),), "weights")
     n, p = e.shape
     if y is None:
-        y = torch.empty((m, p), dtype=e.dtype, device=e.device)
+        y = e.new_empty((m, p))
         ldy = max(p, 1)
         _in_use_on(stream, y)
     else:
@@ -609,6 +615,19 @@ def spsyrk_lookup(ids, e, rowptr=None, weights=None, scale=1.0, y=None, stream=N
     _call(_lib.spsyrk_lookup, "spsyrk_lookup", (ids, e, rowptr, weights, y), stream, m, n, p, nnz, _REAL_CODE[e.dtype], _ptr(rowptr), ids.data_ptr(),
           _ptr(weights), scale, e.data_ptr(), lde, y.data_ptr(), ldy)
     return y
+
+
+@functools.lru_cache(maxsize=256)
+def _lookup_grad_bytes(m, n, p, nnz, code, g_code):
+    sz = ctypes.c_size_t(0)
+    _check(_lib.spsyrk_lookup_grad(m, n, p, nnz, code, g_code, None, None, None, 1.0, None, p, None, p, 0, None, ctypes.byref(sz), None),
+           "spsyrk_lookup_grad(size query)")
+    return sz.value
+
+
+def spsyrk_lookup_grad_workspace_bytes(m, n, p, nnz, dtype, g_dtype=None) -> int:
+    """Bytes that spsyrk_lookup_grad needs for m rows of nnz entries in all, a table of shape (n, p) and dy of `dtype`."""
+    return _lookup_grad_bytes(m, n, p, nnz, _REAL_CODE[dtype], _REAL_CODE[dtype if g_dtype is None else g_dtype])
 
 
 def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None, accumulate=False, dtype=None, workspace=None, stream=None):
@@ -624,21 +643,18 @@ def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None
         dtype = dy.dtype if dtype is None else dtype
         if dtype not in _REAL_CODE:
             raise ValueError(f"{where}: no gradients of {dtype}")
-        de = torch.empty((n, p), dtype=dtype, device=dy.device)
+        de = dy.new_empty((n, p), dtype=dtype)
         ldde = max(p, 1)
         _in_use_on(stream, de)
     else:
         ldde = _matrix(de, where, "de", n, p, dtype)
-    sz = ctypes.c_size_t(0)
     code, g_code = _REAL_CODE[dy.dtype], _REAL_CODE[de.dtype]
-    _check(_lib.spsyrk_lookup_grad(m, n, p, nnz, code, g_code, None, None, None, scale, None, lddy, None, ldde, 0, None, ctypes.byref(sz), None),
-           f"{where}(size query)")
     if workspace is None:
-        workspace = _workspace(sz.value, dy.device)
+        workspace = ids.new_empty(max(_lookup_grad_bytes(m, n, p, nnz, code, g_code), 256), dtype=torch.uint8)
         _in_use_on(stream, workspace)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError(f"{where}: the workspace must be contiguous uint8")
-    sz.value = workspace.numel()
+    sz = ctypes.c_size_t(workspace.numel())
     _call(_lib.spsyrk_lookup_grad, where, (ids, dy, rowptr, weights, de, workspace), stream, m, n, p, nnz, code, g_code, _ptr(rowptr), ids.data_ptr(),
           _ptr(weights), scale, dy.data_ptr(), lddy, de.data_ptr(), ldde, 1 if accumulate else 0, workspace.data_ptr(), ctypes.byref(sz))
     return de
@@ -649,7 +665,7 @@ def spsyrk_lookup_grad_weights(ids, e, dy, rowptr=None, scale=1.0, dw=None, stre
     where = "spsyrk_lookup_grad_weights"
     lde = _matrix(e, where, "e")
     if dw is None:
-        dw = torch.empty(ids.shape, dtype=_weight_dtype(e.dtype), device=e.device)
+        dw = e.new_empty(ids.shape, dtype=_weight_dtype(e.dtype))
         _in_use_on(stream, dw)
     m, nnz = _entries(where, ids, rowptr, dw, (_weight_dtype(e.dtype),), "dw")
     n, p = e.shape
@@ -680,7 +696,9 @@ def _gradient(where, logits, ldl, grad, stream):
     if grad is None or grad is True:
         m, n = logits.shape
         ldg = max(n + (ldl - n) % (16 // logits.element_size()), 1)
-        grad = torch.empty((m, ldg), dtype=logits.dtype, device=logits.device)[:, :n]
+        grad = logits.new_empty((m, ldg))
+        if ldg > n:
+            grad = grad[:, :n]
         _in_use_on(stream, grad)
         return grad, ldg
     return grad, _matrix(grad, where, "grad", *logits.shape, logits.dtype)
@@ -692,9 +710,8 @@ def spsyrk_distill(logits, ids, teacher, rowptr=None, teacher_lse=None, row_weig
     as a third result.  `scale` is temperature^2 unless it is given."""
     where = "spsyrk_distill"
     m, nnz, ldl = _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights)
-    both = torch.empty((2, m), dtype=torch.float32, device=logits.device)
-    _in_use_on(stream, both)
-    loss, lse = both.unbind(0)
+    loss, lse = logits.new_empty(m, dtype=torch.float32), logits.new_empty(m, dtype=torch.float32)
+    _in_use_on(stream, loss, lse)
     with_grad, ldg = grad is not None and grad is not False, 0
     if with_grad:
         grad, ldg = _gradient(where, logits, ldl, grad, stream)

@@ -200,6 +200,8 @@ __global__ void __launch_bounds__(THREADS, 3) lookup_grad_weights_kernel(Rows a,
     const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
     const unsigned mask = lanes == 32 ? FULL_MASK : ((1u << lanes) - 1) << (lane_id() & ~(lanes - 1));
     const int64_t here = (int64_t)(THREADS >> shift) * each, base = (int64_t)blockIdx.x * here;
+    const int64_t t0 = base + (int64_t)(threadIdx.x >> shift) * each, t1 = min(t0 + each, a.nnz);
+    int32_t ahead = t0 + lane < t1 ? ids[t0 + lane] : -1;
     if (a.rowptr) {
         if (threadIdx.x < 64) {
             const int64_t r = a.row_of_by_warp(threadIdx.x < 32 ? base : min(base + here, a.nnz) - 1);
@@ -207,9 +209,9 @@ __global__ void __launch_bounds__(THREADS, 3) lookup_grad_weights_kernel(Rows a,
         }
         __syncthreads();
     }
-    const int64_t t0 = base + (int64_t)(threadIdx.x >> shift) * each, t1 = min(t0 + each, a.nnz);
     for (int64_t t = t0; t < t1; t += lanes) {
-        int32_t my_id = t + lane < t1 ? ids[t + lane] : -1, my_row = 0;
+        int32_t my_id = ahead, my_row = 0;
+        ahead = t + lanes + lane < t1 ? ids[t + lanes + lane] : -1;
         if (my_id >= n || (my_id >= 0 && !a.covered(t + lane))) my_id = -1;
         if (my_id >= 0) my_row = (int32_t)(a.rowptr ? a.row_of(t + lane, span[0], span[1]) : (t + lane) / a.k);
         for (int k = 0; k < lanes && t + k < t1; k += DW_EACH) {

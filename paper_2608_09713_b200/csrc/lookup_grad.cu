@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(THREADS) rank_kernel(Rows a, int64_t n, const 
                                                        uint32_t* __restrict__ key, uint32_t* __restrict__ row, A* __restrict__ weight, int rank_ctas,
                                                        Fill fill) {
     __shared__ __align__(16) uint32_t keys[FEW];
+    __shared__ int64_t span[2];
     const int nnz = (int)a.nnz, lane = lane_id();
     const int64_t from = a.rowptr ? a.rowptr[0] : 0, to = a.rowptr ? a.rowptr[a.m] : a.nnz;
     auto key_of = [&](int t) {
@@ -203,9 +204,13 @@ __global__ void __launch_bounds__(THREADS) rank_kernel(Rows a, int64_t n, const 
 #pragma unroll 8
     for (int t = threadIdx.x; t < up; t += THREADS) keys[t] = t < nnz ? key_of(t) : NO_KEY;  // (behind all others)
     const int t0 = (int)(blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * RANK_EACH;
-    const int64_t my_row = lane < RANK_EACH && t0 + lane < nnz ? a.row_of(t0 + lane, 0, a.m - 1) : 0;  // (while the keys are under way)
+    if (a.rowptr && threadIdx.x < 64) {
+        const int64_t here = (int64_t)blockIdx.x * RANK_HERE, r = a.row_of_by_warp(threadIdx.x < 32 ? here : min(here + RANK_HERE, a.nnz) - 1);
+        if (lane == 0) span[threadIdx.x >> 5] = r;
+    }
     __syncthreads();
     if (t0 >= nnz) return;
+    const int64_t my_row = lane < RANK_EACH && t0 + lane < nnz ? a.rowptr ? a.row_of(t0 + lane, span[0], span[1]) : (t0 + lane) / a.k : 0;
     uint32_t mine[RANK_EACH];
     int before[RANK_EACH] = {};
 #pragma unroll
