@@ -292,6 +292,32 @@ __device__ __forceinline__ double base_in_nats(float base, const Call& c) {
     return (double)base * c.inv_tau_d + (fabsf(base) < LARGE ? ((double)__fmul_rn(base, c.k) - (double)base * (double)c.k) * LN2 : 0.0);
 }
 
+// The gradient of `left` units from `at` on (this thread's: every THREADS-th), but for the teacher's ids: a 2^(s k - shift).  FOLDED: the factor
+// is in the shift already (16-bit results: the approximate logarithm, off by 2^-22, and the shift's rounding are far below their steps).
+template <typename T, bool FOLDED>
+__device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left, float k, float shift, float a) {
+    constexpr int U = 4, PAIRS = Unit<T>::PAIRS;
+    const Pair kk = pair(k, k), off = pair(-shift, -shift), aa = pair(a, a);
+    auto of = [&](const uint4& x) {
+        float2 y[PAIRS];
+#pragma unroll
+        for (int q = 0; q < PAIRS; ++q) {
+            const float2 p = halves(multiply_add(Unit<T>::get(x, q), kk, off));
+            y[q] = float2{power_of_two(p.x), power_of_two(p.y)};
+            if (!FOLDED) y[q] = halves(multiply(pair(y[q].x, y[q].y), aa));
+        }
+        return Unit<T>::put(y);
+    };
+    for (; left >= U * THREADS; left -= U * THREADS, at += U * THREADS, to += U * THREADS) {
+        uint4 x[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) x[i] = __ldcg(at + i * THREADS);
+#pragma unroll
+        for (int i = 0; i < U; ++i) __stcs(to + i * THREADS, of(x[i]));
+    }
+    for (int u = threadIdx.x; u < left; u += THREADS, at += THREADS, to += THREADS) __stcs(to, of(__ldcg(at)));
+}
+
 // Loss and lse of a row, by a whole CTA; the teacher's entries are in shared memory (`few`) or are read again.
 template <typename T>
 __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float weight, int64_t e0, int64_t entries, bool few, const int32_t* s_id,
@@ -349,6 +375,7 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
     __shared__ Joint s_warp[WARPS];
     __shared__ float2 s_cta[8];
     __shared__ int s_again;
+    __shared__ uint64_t s_arrived;
     const uint32_t rank = cluster_rank(), size = 1u << c.log_cluster;
     const int64_t row = blockIdx.x >> c.log_cluster;
     const int tid = threadIdx.x;
@@ -384,7 +411,13 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         return;
     }
 
-    if (size > 1) cluster_arrive();  // (shared memory of a CTA that has not begun is nobody's to write to)
+    if (size > 1) {  // (shared memory of a CTA that has not begun is nobody's to write to)
+        if (tid == 0) {
+            barrier_init(&s_arrived);
+            barrier_init_visible();
+        }
+        cluster_arrive_relaxed();
+    }
 
     if (DISTILL_PREFETCH && tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, mine.units * 16);
 
@@ -410,14 +443,21 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
 
     Running r{-CUDART_INF_F, 0.f};
     if (FORWARD) {
-        const uint4* const from = reinterpret_cast<const uint4*>(s + mine.first);
-        for (int u0 = tid; u0 < mine.units; u0 += U * THREADS) {
+        const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
+        int left = mine.units;
+        for (; left >= U * THREADS; left -= U * THREADS, at += U * THREADS) {  // (nothing to look at: half of the instructions beside the arithmetic)
+            uint4 x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) x[i] = __ldcg(at + i * THREADS);
+            take_units<T, U>(r, x, c.k);
+        }
+        if (tid < left) {
             uint4 x[U];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 constexpr uint32_t none = Unit<T>::NOTHING;
                 x[i] = uint4{none, none, none, none};
-                if (u0 + i * THREADS < mine.units) x[i] = __ldcg(from + u0 + i * THREADS);
+                if (tid + i * THREADS < left) x[i] = __ldcg(at + i * THREADS);
             }
             take_units<T, U>(r, x, c.k);
         }
@@ -443,8 +483,8 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
     teacher = join<WARPS>(joint.teacher, c.k);
     if (size > 1) {
         cluster_wait();
-        if (FORWARD && tid < size) store_to_rank(s_cta + rank, float2{r.most, r.sum}, tid);
-        cluster_arrive();
+        if (tid == 0) barrier_expect(&s_arrived, size * 8);
+        if (tid < size) store_to_rank(s_cta + rank, float2{r.most, r.sum}, &s_arrived, tid);
     }
 
     // meanwhile: an entry for every id of the share; slots of the table hold entries, one of an id's
@@ -475,10 +515,10 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
     auto e_of = [&](float z) { return term(z, top, c.k); };
 
     if (size > 1) {
-        cluster_wait();  // from here on logits may be overwritten: all have fetched the teacher's
+        const bool all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
         if (FORWARD) {
             const float2 part = s_cta[lane_id() & (size - 1)];
-            r = Running{part.x, part.y};
+            r = Running{part.x, all ? part.y : CUDART_NAN_F};  // (a wait that runs out, which should not happen, is seen in the results)
             r = size == 2 ? join<2>(r, c.k) : size == 4 ? join<4>(r, c.k) : join<8>(r, c.k);
         }
     }
@@ -512,40 +552,27 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         const bool plain = fabsf(b) < LARGE;
         auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
         if (few) {
-            {
-                const uint4* const from = reinterpret_cast<const uint4*>(s + mine.first);
+            const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
+            int left = mine.units;
+            const bool folded = sizeof(T) == 2 && plain && a > 0x1p-100f && a < 0x1p100f;
+            const float deep = folded ? shift - __log2f(a) : shift;
+            auto g_of = [&](float x) { return folded ? power_of_two(fmaf(x, c.k, -deep)) : a * q_of(x); };  // the same wherever the rows lie
+            if (plain && aligned) {
+                uint4* to = reinterpret_cast<uint4*>(g + mine.first) + tid;
+                if (folded) write_units<T, true>(at, to, left, c.k, deep, a);
+                else write_units<T, false>(at, to, left, c.k, shift, a);
+            } else {
                 T* const to = g + mine.first;
-                const int units = mine.units;
-                if (plain && aligned) {
-                    const Pair kk = pair(c.k, c.k), off = pair(-shift, -shift), aa = pair(a, a);
-                    for (int u0 = tid; u0 < units; u0 += U * THREADS) {
-                        uint4 x[U];
+                for (int u = tid; u < left; u += THREADS, at += THREADS) {
+                    const uint4 v = __ldcg(at);
+                    const Vec<T, W> x = reinterpret_cast<const Vec<T, W>&>(v);
 #pragma unroll
-                        for (int i = 0; i < U; ++i)
-                            if (u0 + i * THREADS < units) x[i] = DISTILL_LD2(from + u0 + i * THREADS);
-#pragma unroll
-                        for (int i = 0; i < U; ++i) {
-                            if (u0 + i * THREADS >= units) break;
-                            float2 y[PAIRS];
-#pragma unroll
-                            for (int q = 0; q < PAIRS; ++q) {
-                                const float2 p = halves(multiply_add(Unit<T>::get(x[i], q), kk, off));
-                                y[q] = halves(multiply(pair(power_of_two(p.x), power_of_two(p.y)), aa));
-                            }
-                            __stcs(reinterpret_cast<uint4*>(to + (int64_t)(u0 + i * THREADS) * W), Unit<T>::put(y));
-                        }
-                    }
-                } else {
-                    for (int u = tid; u < units; u += THREADS) {
-                        const Vec<T, W> x = *reinterpret_cast<const Vec<T, W>*>(from + u);
-#pragma unroll
-                        for (int q = 0; q < W; ++q) to[(int64_t)u * W + q] = narrow<T>(a * q_of(widen(x.x[q])));
-                    }
+                    for (int q = 0; q < W; ++q) to[(int64_t)u * W + q] = narrow<T>(g_of(widen(x.x[q])));
                 }
             }
             if (rank == 0) {
-                if (tid < mine.head) g[tid] = narrow<T>(a * q_of(widen(s[tid])));
-                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(a * q_of(widen(s[mine.tail + tid])));
+                if (tid < mine.head) g[tid] = narrow<T>(g_of(widen(s[tid])));
+                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
             }
             __syncthreads();
             const bool again = s_again != 0;

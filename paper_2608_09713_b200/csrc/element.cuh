@@ -123,6 +123,8 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
+// (relaxed: says only that this CTA has come so far, and that its barriers in shared memory, made visible, are there)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
@@ -169,10 +171,6 @@ __device__ __forceinline__ void store_to_rank(const float2* mine, float2 v, uint
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(address_in(mine, rank)), "f"(v.x), "f"(v.y),
                  "r"(address_in(bar, rank))
                  : "memory");
-}
-
-__device__ __forceinline__ void store_to_rank(const float2* mine, float2 v, uint32_t rank) {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(address_in(mine, rank)), "f"(v.x), "f"(v.y) : "memory");
 }
 
 }  // namespace spsyrk
