@@ -5,9 +5,9 @@
 // Bound by memory: the logits are read once and the gradient is written once.  A cluster of 1 to 8 CTAs takes a row, each a contiguous
 // share of it: a running maximum and sum per thread, joined over the CTA and the cluster, then the gradient, for which the share is read
 // again.  It is then still in L2 as long as the shares under way are a fraction of it (888 of 64 KB, 57 MB; with rows of 256 KB a CTA, 76 MB and as
-// much of gradients, a third of the reads went to memory again).  A CTA lives some 13 us, most of them latencies, so what counts is how many bytes
-// are under way: six CTAs per SM, and one instruction that asks for the whole share to be brought to L2 before the teacher's entries are
-// looked at (422 us without it, 389 with it for 4096 rows of 131072 bfloat16 logits, 2.1 GB: 84 % of the copy rate).  Kept in shared memory instead
+// much of gradients, many went to memory again).  A CTA lives some 13 us, most of them latencies, so what counts is how many bytes are under
+// way: six CTAs per SM, and one instruction that asks for the whole share to be brought to L2 before the teacher's entries are looked at
+// (422 us without it, 389 with it for 4096 rows of 131072 bfloat16 logits, 2.1 GB; now 373, 88 % of the copy rate).  Kept in shared memory instead
 // of L2 only three shares fit an SM (513 us; with CTAs that stay and copy the next row meanwhile 660, whose rows wait for one another).
 // exp(x) is computed as 2^(s * log2(e) / tau - ...): a multiply-add (two logits per instruction) and an exponential per logit.
 // The gradient is first written for all ids as if they were not the teacher's, then the few of the teacher's are overwritten, from
@@ -23,29 +23,10 @@ using namespace spsyrk;
 
 namespace {
 
-#ifndef DISTILL_THREADS
-#define DISTILL_THREADS 256
-#endif
-#ifndef DISTILL_WARPS_PER_SM
-#define DISTILL_WARPS_PER_SM 48
-#endif
-#ifndef DISTILL_PREFETCH
-#define DISTILL_PREFETCH 1
-#endif
-#ifndef DISTILL_SHARE1
-#define DISTILL_SHARE1 131072
-#endif
-#ifndef DISTILL_LD2
-#define DISTILL_LD2 __ldcg
-#endif
-#ifndef DISTILL_U
-#define DISTILL_U 4
-#endif
-#ifndef DISTILL_SHARE
-#define DISTILL_SHARE 65536
-#endif
-constexpr int THREADS = DISTILL_THREADS;
-constexpr int WARPS = THREADS / 32;
+constexpr int WARPS_PER_SM = 48;
+constexpr int TWICE_SHARE = 65536, ONCE_SHARE = 131072;  // bytes of a row that a CTA takes at most, where it reads them twice and once
+constexpr int SMALL_SHARE = 49152;                       // up to which CTAs have 128 threads instead of 256
+constexpr int ASK_ONCE = 32768;                          // bytes of a share that are asked for at once where it is read once (all where twice)
 constexpr int MOST_TOP = 1024;    // teacher's entries of a row that are kept in shared memory, at most
 constexpr int LEAST_TOP = 32;
 constexpr int WINDOW = 2048;      // ids of a window in rows of more entries
@@ -294,7 +275,7 @@ __device__ __forceinline__ double base_in_nats(float base, const Call& c) {
 
 // The gradient of `left` units from `at` on (this thread's: every THREADS-th), but for the teacher's ids: a 2^(s k - shift).  FOLDED: the factor
 // is in the shift already (16-bit results: the approximate logarithm, off by 2^-22, and the shift's rounding are far below their steps).
-template <typename T, bool FOLDED>
+template <typename T, int THREADS, bool FOLDED>
 __device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left, float k, float shift, float a) {
     constexpr int U = 4, PAIRS = Unit<T>::PAIRS;
     const Pair kk = pair(k, k), off = pair(-shift, -shift), aa = pair(a, a);
@@ -319,9 +300,10 @@ __device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left
 }
 
 // Loss and lse of a row, by a whole CTA; the teacher's entries are in shared memory (`few`) or are read again.
-template <typename T>
+template <typename T, int THREADS>
 __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float weight, int64_t e0, int64_t entries, bool few, const int32_t* s_id,
                                            const float* s_z, const float* s_at, const T* s, Running r, float top, Running teacher) {
+    constexpr int WARPS = THREADS / 32;
     __shared__ double s_sum[WARPS][2];
     const float b = base_of(r.most);
     double mass = 0, cross = 0;  // sum of e_t; of e_t tau (log p_t - log q_t), but for the logarithms that all share
@@ -365,9 +347,9 @@ struct Joint {
 };
 
 // FORWARD: the sum over the row is computed (else it is `kept`); GRAD: the gradient is written.
-template <typename T, bool FORWARD, bool GRAD>
-__global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) distill_kernel(const Call c, const T* logits, T* grad) {
-    constexpr int W = 16 / (int)sizeof(T), U = DISTILL_U, PAIRS = Unit<T>::PAIRS;
+template <typename T, int THREADS, bool FORWARD, bool GRAD>
+__global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_kernel(const Call c, const T* logits, T* grad) {
+    constexpr int W = 16 / (int)sizeof(T), U = 4, WARPS = THREADS / 32;
     extern __shared__ int32_t windows[];  // rows of many entries: [WINDOW]; else the teacher's entries
     int32_t* const s_id = windows;  // [top]
     float *const s_z = reinterpret_cast<float*>(s_id + c.top), *const s_at = s_z + c.top;  // [top] the teacher's logit, the student's
@@ -419,7 +401,7 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         cluster_arrive_relaxed();
     }
 
-    if (DISTILL_PREFETCH && tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, mine.units * 16);
+    if (tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, FORWARD && GRAD ? mine.units * 16 : min(mine.units * 16, ASK_ONCE));
 
     // the teacher's row
     Running teacher{-CUDART_INF_F, 0.f};
@@ -523,7 +505,7 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
         }
     }
     if (!few && FORWARD) {  // the loss needs logits that the gradient may overwrite
-        if (rank == 0) write_loss(c, row, weight, e0, entries, false, s_id, s_z, s_at, s, r, top, teacher);
+        if (rank == 0) write_loss<T, THREADS>(c, row, weight, e0, entries, false, s_id, s_z, s_at, s, r, top, teacher);
         if (size > 1) {
             cluster_arrive();
             cluster_wait();
@@ -559,8 +541,8 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
             auto g_of = [&](float x) { return folded ? power_of_two(fmaf(x, c.k, -deep)) : a * q_of(x); };  // the same wherever the rows lie
             if (plain && aligned) {
                 uint4* to = reinterpret_cast<uint4*>(g + mine.first) + tid;
-                if (folded) write_units<T, true>(at, to, left, c.k, deep, a);
-                else write_units<T, false>(at, to, left, c.k, shift, a);
+                if (folded) write_units<T, THREADS, true>(at, to, left, c.k, deep, a);
+                else write_units<T, THREADS, false>(at, to, left, c.k, shift, a);
             } else {
                 T* const to = g + mine.first;
                 for (int u = tid; u < left; u += THREADS, at += THREADS) {
@@ -617,18 +599,13 @@ __global__ void __launch_bounds__(THREADS, DISTILL_WARPS_PER_SM * 32 / THREADS) 
             }
         }
     }
-    if (FORWARD && few && rank == 0) write_loss(c, row, weight, e0, entries, true, s_id, s_z, s_at, s, r, top, teacher);
+    if (FORWARD && few && rank == 0) write_loss<T, THREADS>(c, row, weight, e0, entries, true, s_id, s_z, s_at, s, r, top, teacher);
 }
 
-template <typename T, bool FORWARD, bool GRAD>
-spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) {
-    constexpr int W = 16 / (int)sizeof(T);
-    constexpr auto kernel = distill_kernel<T, FORWARD, GRAD>;
-    const int64_t units = (c.n + W - 1) / W;
-    // shares of at most DISTILL_SHARE bytes; smaller ones, down to 16 KB, as long as the CTAs do not fill the GPU
-    int cluster = 1;
-    while (cluster < 8 && (units > cluster * ((FORWARD && GRAD ? DISTILL_SHARE : DISTILL_SHARE1) / 16) || (c.rows.m * cluster < 3 * SMS && units >= cluster * 1024))) cluster *= 2, ++c.log_cluster;
-    if (c.rows.m * cluster >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
+template <typename T, int THREADS, bool FORWARD, bool GRAD>
+spsyrk_status_t launch_by(Call c, const void* logits, void* grad, cudaStream_t st) {
+    constexpr auto kernel = distill_kernel<T, THREADS, FORWARD, GRAD>;
+    const int cluster = 1 << c.log_cluster;
     // entries in shared memory: all if every row has as many, else room for four times the mean
     const int64_t entries = c.rows.rowptr ? std::max<int64_t>(128, 4 * (c.rows.nnz / c.rows.m)) : c.rows.k;
     c.top = LEAST_TOP;
@@ -650,6 +627,19 @@ spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) 
     cfg.numAttrs = 1;
     SPSYRK_CUDA_TRY(launch_kernel(cfg, kernel, Call(c), static_cast<const T*>(logits), static_cast<T*>(grad)));
     return SPSYRK_OK;
+}
+
+template <typename T, bool FORWARD, bool GRAD>
+spsyrk_status_t launch(Call c, const void* logits, void* grad, cudaStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const int64_t units = (c.n + W - 1) / W;
+    // smaller shares, down to 16 KB, as long as the CTAs do not fill the GPU
+    constexpr int64_t MOST = (FORWARD && GRAD ? TWICE_SHARE : ONCE_SHARE) / 16;
+    while (c.log_cluster < 3 && (units > MOST << c.log_cluster || (c.rows.m << c.log_cluster < 3 * SMS && units >= int64_t(1024) << c.log_cluster))) ++c.log_cluster;
+    if (c.rows.m << c.log_cluster >= int64_t(1) << 31) return SPSYRK_ERR_OVERFLOW;
+    // Many short rows: the latencies of a row hide behind more rows, of fewer warps each (8000 rows of 8192 bfloat16 logits 76 us against 86, 4000 of
+    // 3001 half-precision ones 37 against 47).
+    return (units >> c.log_cluster) * 16 <= SMALL_SHARE && c.rows.m > 6 * SMS ? launch_by<T, 128, FORWARD, GRAD>(c, logits, grad, st) : launch_by<T, 256, FORWARD, GRAD>(c, logits, grad, st);
 }
 
 bool is_logit(spsyrk_dtype_t t) { return t == SPSYRK_F32 || t == SPSYRK_BF16 || t == SPSYRK_F16; }

@@ -49,13 +49,14 @@ __global__ void __launch_bounds__(THREADS) lookup_one_kernel(int64_t m, int64_t 
 
 // acc += the weighted rows of entries [b, end) at column c, UNROLL rows under way at a time.  The lanes of a group (those of it that
 // share a warp) fetch an id and a weight each and hand them round; the next ones are under way meanwhile.
-constexpr int UNROLL = 8;
+// (eight sums a lane leave registers for four rows of 16 bytes at a time, fewer sums for eight)
+template <int V> constexpr int UNROLL = V == 8 ? 4 : 8;
 template <typename T, int V>
 __device__ __forceinline__ void add_entries(int64_t b, int64_t end, int64_t n, int64_t p, int64_t c, const int32_t* __restrict__ ids,
                                             const typename Wide<T>::type* __restrict__ weights, const T* __restrict__ e, int64_t lde, int shift,
                                             typename Wide<T>::type (&acc)[V]) {
     using A = typename Wide<T>::type;
-    constexpr int U = UNROLL;
+    constexpr int U = UNROLL<V>;
     const int share = 1 << min(shift, 5), lane = threadIdx.x & (share - 1);
     const unsigned mask = share == 32 ? FULL_MASK : ((1u << share) - 1) << (lane_id() & ~(share - 1));
     int32_t next_id = -1;
@@ -95,27 +96,39 @@ __device__ __forceinline__ void add_entries(int64_t b, int64_t end, int64_t n, i
     }
 }
 
-// A group per row; rows of more than `longest` entries are left to lookup_long_kernel.
-template <typename T, int V>
+// A group per row; rows of more than `longest` entries are left to lookup_long_kernel.  Few narrow rows: 1 << split groups of a warp share a row,
+// each takes a contiguous share of the entries.
+template <typename T, int V, bool SHARED>
 __global__ void __launch_bounds__(THREADS, 3) lookup_rows_kernel(Rows a, int64_t n, int64_t p, const int32_t* __restrict__ ids,
-                                                              const typename Wide<T>::type* __restrict__ weights, typename Wide<T>::type scale,
-                                                              const T* __restrict__ e, int64_t lde, T* __restrict__ y, int64_t ldy, int shift,
-                                                              int64_t longest) {
+                                                                 const typename Wide<T>::type* __restrict__ weights, typename Wide<T>::type scale,
+                                                                 const T* __restrict__ e, int64_t lde, T* __restrict__ y, int64_t ldy, int shift, int split,
+                                                                 int64_t longest) {
     using A = typename Wide<T>::type;
     chain_begin();
-    const int64_t row = (int64_t)blockIdx.x * (THREADS >> shift) + (threadIdx.x >> shift);
-    const int lane = threadIdx.x & ((1 << shift) - 1);
+    if (!SHARED) split = 0;
+    const int all = shift + split;  // at most 5 if split > 0
+    const int64_t row = (int64_t)blockIdx.x * (THREADS >> all) + (threadIdx.x >> all);
+    const int lane = threadIdx.x & ((1 << shift) - 1), part = (threadIdx.x >> shift) & ((1 << split) - 1);
+    const unsigned mask = all >= 5 ? FULL_MASK : ((1u << (1 << all)) - 1) << (lane_id() & ~((1 << all) - 1));
     if (row < a.m) {
-        const int64_t b = a.begin(row), end = a.end(row);
-        if (end - b <= longest) {
+        const int64_t begin = a.begin(row), len = a.end(row) - begin;
+        if (len <= longest) {
+            const int64_t each = (max(len, (int64_t)0) + (1 << split) - 1) >> split, b = begin + min(len, part * each), end = begin + min(len, (part + 1) * each);
             // (all lanes of a group stay together: they hand ids round)
             for (int64_t c0 = 0; c0 < p; c0 += (int64_t)V << shift) {
                 const int64_t c = c0 + (int64_t)lane * V;
                 A acc[V] = {};
                 add_entries<T, V>(b, end, n, p, c, ids, weights, e, lde, shift, acc);
+                if (SHARED) {
+                    __syncwarp(mask);
+                    for (int s = 0; s < split; ++s) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[i] += __shfl_xor_sync(mask, acc[i], 1 << (shift + s));
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] *= scale;
-                if (c < p) store_narrow<T, V>(y + row * ldy + c, p - c, acc);
+                if (part == 0 && c < p) store_narrow<T, V>(y + row * ldy + c, p - c, acc);
             }
         }
     }
@@ -232,17 +245,20 @@ __global__ void __launch_bounds__(THREADS, 3) lookup_grad_weights_kernel(Rows a,
             if (the_row >= 0) {
                 for (int64_t c = (int64_t)lane * V; c < p; c += (int64_t)V << shift) {
                     A g[V];
-                    Vec<T, V> x[DW_EACH];
-#pragma unroll
-                    for (int u = 0; u < DW_EACH; ++u)
-                        if (id[u] >= 0) x[u] = load_raw<T, V>(e + id[u] * lde + c, p - c);
                     if (same) load_wide<T, V>(dy + the_row * lddy + c, p - c, g);
 #pragma unroll
-                    for (int u = 0; u < DW_EACH; ++u) {
-                        if (!same) load_wide<T, V>(id[u] >= 0 ? dy + row[u] * lddy + c : dy, id[u] >= 0 ? p - c : 0, g);
-                        if (id[u] < 0) continue;
+                    for (int h = 0; h < DW_EACH; h += DW_EACH / 2) {  // (half of the entries at a time: registers)
+                        Vec<T, V> x[DW_EACH / 2];
 #pragma unroll
-                        for (int i = 0; i < V; ++i) dot[u] += widen(x[u].x[i]) * g[i];
+                        for (int u = 0; u < DW_EACH / 2; ++u)
+                            if (id[h + u] >= 0) x[u] = load_raw<T, V>(e + id[h + u] * lde + c, p - c);
+#pragma unroll
+                        for (int u = 0; u < DW_EACH / 2; ++u) {
+                            if (!same) load_wide<T, V>(id[h + u] >= 0 ? dy + row[h + u] * lddy + c : dy, id[h + u] >= 0 ? p - c : 0, g);
+                            if (id[h + u] < 0) continue;
+#pragma unroll
+                            for (int i = 0; i < V; ++i) dot[h + u] += widen(x[u].x[i]) * g[i];
+                        }
                     }
                 }
             }
@@ -296,9 +312,15 @@ spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t*
     // 64 of them run at a time.  So few rows go to clusters from 128 entries on, of many only those far above the mean.
     const int64_t longest = a.m <= 4 * LONG_UNITS ? 128 : std::max<int64_t>(512, 4 * (a.nnz / a.m));
     Chain chain{st, true};
-    if (a.rowptr || a.k <= longest)
-        SPSYRK_CUDA_TRY(chain.launch(true, lookup_rows_kernel<T, V>, (unsigned)((a.m + per_cta - 1) / per_cta), THREADS, 0, a, n, p, ids, wv, (A)scale, ev, lde, yv,
-                                     ldy, shift, longest));
+    if (a.rowptr || a.k <= longest) {
+        // rows are shared while they do not fill every SM with threads and have eight entries for everyone
+        int split = 0;
+        while (shift + split < 5 && a.m << (shift + split) < (int64_t)SMS * 2048 && a.nnz / a.m >= int64_t(16) << split) ++split;
+        const int64_t rows = THREADS >> (shift + split);
+        const auto kernel = split ? lookup_rows_kernel<T, V, true> : lookup_rows_kernel<T, V, false>;
+        SPSYRK_CUDA_TRY(chain.launch(true, kernel, (unsigned)((a.m + rows - 1) / rows), THREADS, 0, a, n, p, ids, wv, (A)scale, ev, lde, yv,
+                                     ldy, shift, split, longest));
+    }
     if (a.rowptr ? a.nnz > longest : a.k > longest) {
         const int64_t units = std::min<int64_t>(LONG_UNITS, a.m);
         // slabs of at most 64 lanes, for more CTAs
