@@ -450,6 +450,7 @@ spsyrk_status_t spsyrk_lookup_grad_weights(int64_t m, int64_t n, int64_t p, int6
  * lse are 0, its gradient is 0, its logits are not looked at.  NaN or +infinity among the logits that a row is computed from, the student's
  * or the teacher's, make its loss and its whole gradient NaN, and so do a student's logits that are all -infinity.
  * d_loss[m] and d_lse[m] are float and may be NULL; G is m x n of `dtype`, NULL: no gradient, else computed in the same pass.
+ * (Sums with and without G are taken in different orders: last bits of loss and lse may differ between the two.)
  * G may be s itself (same stride), else it must not alias s.
  */
 spsyrk_status_t spsyrk_distill(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t teacher_dtype,

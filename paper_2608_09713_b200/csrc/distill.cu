@@ -26,7 +26,7 @@ namespace {
 constexpr int WARPS_PER_SM = 48;
 constexpr int TWICE_SHARE = 65536, ONCE_SHARE = 131072;  // bytes of a row that a CTA takes at most, where it reads them twice and once
 constexpr int SMALL_SHARE = 49152;                       // up to which CTAs have 128 threads instead of 256
-constexpr int ASK_ONCE = 32768;                          // bytes of a share that are asked for at once where it is read once (all where twice)
+constexpr int ASK_ONCE = 32768;                          // bytes of a share that are asked for at once where it is read once (all but in the widest rows where twice)
 constexpr int MOST_TOP = 1024;    // teacher's entries of a row that are kept in shared memory, at most
 constexpr int LEAST_TOP = 32;
 constexpr int WINDOW = 2048;      // ids of a window in rows of more entries
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
         cluster_arrive_relaxed();
     }
 
-    if (tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, FORWARD && GRAD ? mine.units * 16 : min(mine.units * 16, ASK_ONCE));
+    if (tid == 0 && (FORWARD || few) && mine.units > 0) prefetch(s + mine.first, min(mine.units * 16, FORWARD && GRAD ? 2 * TWICE_SHARE : ASK_ONCE));
 
     // the teacher's row
     Running teacher{-CUDART_INF_F, 0.f};

@@ -309,8 +309,9 @@ spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t*
         return SPSYRK_OK;
     }
     // A group reads a row eight entries at a time, about a microsecond each; a cluster spends some 3 us on a row beside its loads and
-    // 64 of them run at a time.  So few rows go to clusters from 128 entries on, of many only those far above the mean.
-    const int64_t longest = a.m <= 4 * LONG_UNITS ? 128 : std::max<int64_t>(512, 4 * (a.nnz / a.m));
+    // 64 of them run at a time.  So few rows go to clusters from 128 entries on, more rows from 512 on, and of rows that fill the GPU by themselves
+    // only those far above the mean.
+    const int64_t longest = a.m <= 4 * LONG_UNITS ? 128 : a.m << shift < (int64_t)SMS * 1024 ? 512 : std::max<int64_t>(512, 4 * (a.nnz / a.m));
     Chain chain{st, true};
     if (a.rowptr || a.k <= longest) {
         // rows are shared while they do not fill every SM with threads and have eight entries for everyone
@@ -402,9 +403,13 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad_weights(int64_t m, int64_t n, int6
     if (s != SPSYRK_OK) return s;
     if (!is_real(dtype) || lde < p || lddy < p) return SPSYRK_ERR_INVALID_ARG;
     if (nnz == 0) return SPSYRK_OK;
-    if (m == 0 || !d_dw || (n > 0 && p > 0 && (!d_e || !d_dy))) return SPSYRK_ERR_INVALID_ARG;
+    if (!d_dw || (m > 0 && n > 0 && p > 0 && (!d_e || !d_dy))) return SPSYRK_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const size_t size = element_size(dtype);
+    if (m == 0) {  // entries of no row
+        SPSYRK_CUDA_TRY(cudaMemsetAsync(d_dw, 0, (size_t)nnz * (dtype == SPSYRK_F64 ? 8 : 4), st));
+        return SPSYRK_OK;
+    }
     const bool wide = aligned16(d_e, lde, size) && aligned16(d_dy, lddy, size);
 #define CALL(T, V) (grad_weights_typed<T, V>(a, n, p, d_ids, scale, d_e, lde, d_dy, lddy, d_dw, st))
     SPSYRK_BY_TYPE(dtype, wide, CALL)

@@ -533,10 +533,10 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     if (lddy < p || ldde < p || (nnz > 0 && !d_ids)) return SPSYRK_ERR_INVALID_ARG;
     if (!d_rowptr && (m == 0 ? nnz != 0 : nnz % m != 0)) return SPSYRK_ERR_INVALID_ARG;
     if (n == 0 || p == 0) return SPSYRK_OK;
-    if (!d_de || (nnz > 0 && (m == 0 || !d_dy))) return SPSYRK_ERR_INVALID_ARG;
+    if (!d_de || (nnz > 0 && m > 0 && !d_dy)) return SPSYRK_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const size_t size = element_size(dtype), g_size = element_size(g_dtype);
-    if (nnz == 0) {
+    if (nnz == 0 || m == 0) {  // (entries of no row)
         if (!accumulate) SPSYRK_CUDA_TRY(cudaMemset2DAsync(d_de, (size_t)ldde * g_size, 0, (size_t)p * g_size, (size_t)n, st));
         return SPSYRK_OK;
     }

@@ -180,6 +180,29 @@ def test_entries_of_no_row(B):
         V.check_grad_weights(B.spsyrk_lookup_grad_weights(ids, e, dy, rowptr=rowptr), ids, e, dy, rowptr, 1.0)
 
 
+def test_no_rows_but_entries(B):
+    rowptr, ids = torch.tensor([3], device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda")
+    e, dy = torch.ones((9, 8), device="cuda"), torch.ones((0, 8), device="cuda")
+    assert B.spsyrk_lookup(ids, e, rowptr=rowptr).shape == (0, 8)
+    de = torch.ones((9, 8), device="cuda")
+    B.spsyrk_lookup_grad(ids, dy, 9, rowptr=rowptr, de=de, accumulate=True)
+    assert (de == 1).all()
+    assert (B.spsyrk_lookup_grad(ids, dy, 9, rowptr=rowptr) == 0).all()
+    assert (B.spsyrk_lookup_grad_weights(ids, e, dy, rowptr=rowptr) == 0).all()
+
+
+@pytest.mark.parametrize("m,k,p", [(300, 900, 64), (300, 900, 20), (257, 130, 8), (1000, 600, 16), (3, 20_000, 100), (400, 33, 2000)])
+def test_rows_of_every_way(B, m, k, p):
+    """Shared by the groups of a warp, by clusters, one group each: fixed and ragged rows."""
+    gen = _gen(m + k)
+    ids, w = _ids(m * k, 5000, gen), _weights(m * k, torch.float32, gen)
+    e, _ = V.matrix(5000, p, torch.float32, gen)
+    V.check_lookup(B.spsyrk_lookup(ids.view(m, k), e, weights=w.view(m, k)), ids, e, torch.arange(m + 1, device="cuda") * k, w, 1.0)
+    length = torch.randint(0, 2 * k, (m,), generator=gen, device="cuda").cumsum(0)
+    rowptr = torch.cat((torch.zeros(1, dtype=torch.int64, device="cuda"), length)).clamp(max=m * k)
+    V.check_lookup(B.spsyrk_lookup(ids, e, rowptr=rowptr, weights=w), ids, e, rowptr, w, 1.0)
+
+
 def test_nothing_to_do(B):
     none = torch.empty(0, dtype=torch.int32, device="cuda")
     for dtype in V.DTYPES:
