@@ -92,6 +92,7 @@ struct Fill {
     int size;                       // of an element
     int64_t rows;                   // a CTA's
     int64_t n;
+    bool aligned;                   // rows begin and end at 16-byte boundaries
     template <typename Present>
     __device__ __forceinline__ void rows_of(int64_t v0, int64_t v1, Present present) const {
         const int shift = min(5, 32 - __clz((int)min((used_bytes + 15) / 16, (int64_t)32) - 1));
@@ -100,6 +101,15 @@ struct Fill {
         for (int64_t first = v0 + (int64_t)(threadIdx.x >> 5) * each; first < v1; first += (int64_t)warps * each) {
             const int count = (int)min((int64_t)each, v1 - first);
             const unsigned taken = __ballot_sync(FULL_MASK, lane_id() < count && present(first + lane_id()));
+            if (aligned) {  // (the ends of a row, if they have to be looked for, take more instructions than the row where it is narrow)
+                const int units = (int)(used_bytes / 16), rows_a_step = 32 >> shift;
+                char* at = de + (first + (lane_id() >> shift)) * row_bytes + lane * 16;
+                for (int r = lane_id() >> shift; r < count; r += rows_a_step, at += row_bytes * rows_a_step) {
+                    if (taken >> r & 1u) continue;
+                    for (int c = lane; c < units; c += lanes) *reinterpret_cast<uint4*>(at + (int64_t)(c - lane) * 16) = uint4{0, 0, 0, 0};
+                }
+                continue;
+            }
             for (int r = lane_id() >> shift; r < count; r += 32 >> shift) {
                 if (taken >> r & 1u) continue;
                 char* const at = de + (first + r) * row_bytes;
@@ -545,7 +555,8 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     carve(&w, d_workspace, n, p, nnz, dtype == SPSYRK_F64, true);
     // 256 KB of dE a CTA, at most 512 rows
     const int64_t used = p * (int64_t)g_size;
-    Fill fill{static_cast<char*>(d_de), ldde * (int64_t)g_size, used, (int)g_size, accumulate ? 0 : std::max<int64_t>(1, std::min<int64_t>(512, (1 << 18) / used)), n};
+    Fill fill{static_cast<char*>(d_de), ldde * (int64_t)g_size, used, (int)g_size, accumulate ? 0 : std::max<int64_t>(1, std::min<int64_t>(512, (1 << 18) / used)), n,
+              reinterpret_cast<uintptr_t>(d_de) % 16 == 0 && ldde * (int64_t)g_size % 16 == 0 && used % 16 == 0};
     int which = 0;
     const spsyrk_status_t s = dtype == SPSYRK_F64 ? order_entries<double>(w, a, n, d_ids, d_weights, &fill, &which, st)
                                                   : order_entries<float>(w, a, n, d_ids, d_weights, &fill, &which, st);
