@@ -357,6 +357,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     __shared__ Joint s_warp[WARPS];
     __shared__ float2 s_cta[8];
     __shared__ int s_again;
+    __shared__ uint32_t s_more[MOST_TOP / 32];  // a bit per entry: others have its id too
     __shared__ uint64_t s_arrived;
     const uint32_t rank = cluster_rank(), size = 1u << c.log_cluster;
     const int64_t row = blockIdx.x >> c.log_cluster;
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     constexpr uint16_t NO_ENTRY = 0xffff;
     if (GRAD && few) {
         for (int i = tid; i < slots; i += THREADS) table[i] = NO_ENTRY;
-        if (tid == 0) s_again = 0;
+        if (tid < MOST_TOP / 32) s_more[tid] = 0;
     }
 
     Running r{-CUDART_INF_F, 0.f};
@@ -484,7 +485,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
                     break;
                 }
                 if (s_id[was] == id) {
-                    s_again = 1;
+                    atomicOr(&s_more[was >> 5], 1u << (was & 31));
                     break;
                 }
             }
@@ -557,12 +558,11 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
                 if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
             }
             __syncthreads();
-            const bool again = s_again != 0;
             for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {
                 if (!(chosen >> bit & 1u)) continue;
                 const int32_t id = s_id[t];
                 float e = e_of(s_z[t]);
-                if (again) {
+                if (s_more[t >> 5] >> (t & 31) & 1u) {
                     e = 0.f;
                     for (int o = 0; o < count; ++o)
                         if (s_id[o] == id) e += e_of(s_z[o]);

@@ -79,7 +79,11 @@ __device__ __forceinline__ void store_narrow(T* __restrict__ p, int64_t left, co
 
 inline size_t element_size(spsyrk_dtype_t t) { return t == SPSYRK_F64 ? 8 : t == SPSYRK_BF16 || t == SPSYRK_F16 ? 2 : 4; }
 inline bool is_real(spsyrk_dtype_t t) { return t == SPSYRK_F64 || t == SPSYRK_F32 || t == SPSYRK_BF16 || t == SPSYRK_F16; }
-inline bool aligned16(const void* p, int64_t ld, size_t size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)size % 16 == 0; }
+// Elements that can be read and written together in every row of a matrix: 16 bytes, or two elements, or one.
+inline int together(const void* p, int64_t ld, size_t size) {
+    const uint64_t bits = (uint64_t)reinterpret_cast<uintptr_t>(p) | (uint64_t)ld * size;
+    return bits % 16 == 0 ? (int)(16 / size) : bits % (2 * size) == 0 ? 2 : 1;
+}
 
 // Rows of entries: row pointers, or the same number of entries k in every row.  Row pointers are cut to [0, nnz], so that no
 // entry is looked for outside the arrays whatever they hold.

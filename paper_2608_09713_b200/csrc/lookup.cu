@@ -16,6 +16,10 @@ constexpr int SMS = 148;
 constexpr int LONG_CLUSTER = 8;
 constexpr int LONG_UNITS = 64;  // clusters that look for long rows
 
+// Where rows are gathered entry by entry, two 16-bit elements at a time are slower than one (2500 sets of 40 of 1002 bfloat16 columns 176 us against
+// 143, the gradient of their weights 141 against 129); two floats are faster (90 against 150, 100 against 166).
+template <typename T, int V> constexpr int BY_ENTRIES = V == 2 && sizeof(T) == 2 ? 1 : V;
+
 // lanes of a group: a power of two that covers the row's vectors, at most a CTA
 int group_shift(int64_t vectors) {
     int s = 0;
@@ -293,8 +297,9 @@ __global__ void __launch_bounds__(THREADS, 3) lookup_grad_weights_kernel(Rows a,
     }
 }
 
+// Rows of one id each.
 template <typename T, int V>
-spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t* ids, const void* weights, double scale, const void* e, int64_t lde,
+spsyrk_status_t lookup_one_typed(const Rows& a, int64_t n, int64_t p, const int32_t* ids, const void* weights, double scale, const void* e, int64_t lde,
                              void* y, int64_t ldy, cudaStream_t st) {
     using A = typename Wide<T>::type;
     const A* wv = static_cast<const A*>(weights);
@@ -302,12 +307,21 @@ spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t*
     T* yv = static_cast<T*>(y);
     const int shift = group_shift((p + V - 1) / V);
     const int64_t per_cta = THREADS >> shift;
-    if (!a.rowptr && a.k == 1) {
-        lookup_one_kernel<T, V><<<(unsigned)((a.m + per_cta - 1) / per_cta), THREADS, 0, st>>>(a.m, n, p, ids, wv, (A)scale, ev, lde, yv, ldy, shift);
-        note_launches(1);
-        SPSYRK_CUDA_TRY(cudaGetLastError());
-        return SPSYRK_OK;
-    }
+    lookup_one_kernel<T, V><<<(unsigned)((a.m + per_cta - 1) / per_cta), THREADS, 0, st>>>(a.m, n, p, ids, wv, (A)scale, ev, lde, yv, ldy, shift);
+    note_launches(1);
+    SPSYRK_CUDA_TRY(cudaGetLastError());
+    return SPSYRK_OK;
+}
+
+// Rows of any number.
+template <typename T, int V>
+spsyrk_status_t lookup_rows_typed(const Rows& a, int64_t n, int64_t p, const int32_t* ids, const void* weights, double scale, const void* e, int64_t lde,
+                             void* y, int64_t ldy, cudaStream_t st) {
+    using A = typename Wide<T>::type;
+    const A* wv = static_cast<const A*>(weights);
+    const T* ev = static_cast<const T*>(e);
+    T* yv = static_cast<T*>(y);
+    const int shift = group_shift((p + V - 1) / V);
     // A group reads a row eight entries at a time, about a microsecond each; a cluster spends some 3 us on a row beside its loads and
     // 64 of them run at a time.  So few rows go to clusters from 128 entries on, more rows from 512 on, and of rows that fill the GPU by themselves
     // only those far above the mean.
@@ -342,6 +356,14 @@ spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t*
 }
 
 template <typename T, int V>
+spsyrk_status_t lookup_typed(const Rows& a, int64_t n, int64_t p, const int32_t* ids, const void* weights, double scale, const void* e, int64_t lde,
+                             void* y, int64_t ldy, cudaStream_t st) {
+    // (two floats at a time copy no faster than one: 20000 rows of 1002 51 us against 45)
+    if (!a.rowptr && a.k == 1) return lookup_one_typed<T, V == 2 && sizeof(T) == 4 ? 1 : V>(a, n, p, ids, weights, scale, e, lde, y, ldy, st);
+    return lookup_rows_typed<T, BY_ENTRIES<T, V>>(a, n, p, ids, weights, scale, e, lde, y, ldy, st);
+}
+
+template <typename T, int V>
 spsyrk_status_t grad_weights_typed(const Rows& a, int64_t n, int64_t p, const int32_t* ids, double scale, const void* e, int64_t lde, const void* dy,
                                    int64_t lddy, void* dw, cudaStream_t st) {
     using A = typename Wide<T>::type;
@@ -369,13 +391,13 @@ spsyrk_status_t check_rows(int64_t m, int64_t n, int64_t p, int64_t nnz, const i
 
 }  // namespace
 
-// a typed call, 16 bytes at a time if everything is aligned to that
-#define SPSYRK_BY_TYPE(dtype, wide, call)                                               \
-    switch (dtype) {                                                                    \
-        case SPSYRK_F64: return wide ? call(double, 2) : call(double, 1);               \
-        case SPSYRK_F32: return wide ? call(float, 4) : call(float, 1);                 \
-        case SPSYRK_BF16: return wide ? call(__nv_bfloat16, 8) : call(__nv_bfloat16, 1); \
-        default: return wide ? call(__half, 8) : call(__half, 1);                       \
+// a typed call with as many elements together as all matrices allow (8, 4 or 2 for 2-, 4- and 8-byte elements; 2; 1)
+#define SPSYRK_BY_TYPE(dtype, width, call)                                                                                               \
+    switch (dtype) {                                                                                                                     \
+        case SPSYRK_F64: return width >= 2 ? call(double, 2) : call(double, 1);                                                          \
+        case SPSYRK_F32: return width >= 4 ? call(float, 4) : width == 2 ? call(float, 2) : call(float, 1);                              \
+        case SPSYRK_BF16: return width >= 8 ? call(__nv_bfloat16, 8) : width == 2 ? call(__nv_bfloat16, 2) : call(__nv_bfloat16, 1);     \
+        default: return width >= 8 ? call(__half, 8) : width == 2 ? call(__half, 2) : call(__half, 1);                                   \
     }
 
 extern "C" spsyrk_status_t spsyrk_lookup(int64_t m, int64_t n, int64_t p, int64_t nnz, spsyrk_dtype_t dtype, const int64_t* d_rowptr,
@@ -389,9 +411,9 @@ extern "C" spsyrk_status_t spsyrk_lookup(int64_t m, int64_t n, int64_t p, int64_
     if (!d_y || (n > 0 && nnz > 0 && !d_e)) return SPSYRK_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const size_t size = element_size(dtype);
-    const bool wide = aligned16(d_e, lde, size) && aligned16(d_y, ldy, size);
+    const int width = std::min(together(d_e, lde, size), together(d_y, ldy, size));
 #define CALL(T, V) (lookup_typed<T, V>(a, n, p, d_ids, d_weights, scale, d_e, lde, d_y, ldy, st))
-    SPSYRK_BY_TYPE(dtype, wide, CALL)
+    SPSYRK_BY_TYPE(dtype, width, CALL)
 #undef CALL
 }
 
@@ -410,8 +432,8 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad_weights(int64_t m, int64_t n, int6
         SPSYRK_CUDA_TRY(cudaMemsetAsync(d_dw, 0, (size_t)nnz * (dtype == SPSYRK_F64 ? 8 : 4), st));
         return SPSYRK_OK;
     }
-    const bool wide = aligned16(d_e, lde, size) && aligned16(d_dy, lddy, size);
-#define CALL(T, V) (grad_weights_typed<T, V>(a, n, p, d_ids, scale, d_e, lde, d_dy, lddy, d_dw, st))
-    SPSYRK_BY_TYPE(dtype, wide, CALL)
+    const int width = std::min(together(d_e, lde, size), together(d_dy, lddy, size));
+#define CALL(T, V) (grad_weights_typed<T, BY_ENTRIES<T, V>>(a, n, p, d_ids, scale, d_e, lde, d_dy, lddy, d_dw, st))
+    SPSYRK_BY_TYPE(dtype, width, CALL)
 #undef CALL
 }

@@ -53,6 +53,7 @@ def _rowptr(lengths, before=0):
 SHAPES = [
     (1, 1, 1, 1, 0, 0), (16, 1, 300, 1024, 0, 0), (1000, 1, 77, 64, 8, 0), (333, 1, 200, 1001, 0, 0), (40, 1, 50, 4096, 0, 1), (20_000, 1, 100, 72, 0, 0),
     (9, 1, 10, 5, 3, 0), (3, 1, 2, 9000, 0, 0), (50, 3, 60, 64, 0, 0), (7, 200, 90, 33, 1, 0), (300, 40, 500, 256, 0, 0), (2, 1500, 400, 136, 0, 0),
+    (333, 1, 200, 1002, 0, 0), (50, 5, 90, 70, 0, 2), (40, 1, 50, 30, 4, 0), ("short", None, 30, 66, 0, 0), ("long", None, 200, 502, 0, 0),
     ("short", None, 30, 64, 0, 0), ("long", None, 500, 7, 0, 0), ("long", None, 300, 520, 8, 8), ("one", None, 20, 2000, 0, 0), ("none", None, 9, 16, 0, 0),
     ("many", None, 1000, 48, 0, 0), ("many with long ones", None, 400, 100, 0, 0), ("many", None, 3, 1, 0, 0),
 ]
@@ -125,7 +126,7 @@ def test_gradients(B, shape, dtype, weighted):
 
 
 @pytest.mark.parametrize("weighted", [False, True])
-@pytest.mark.parametrize("count,n,p", [(8192, 300, 40), (8193, 300, 40), (8193, 255, 16), (8193, 256, 16), (30_000, 70_000, 24), (100_001, 1, 65),
+@pytest.mark.parametrize("count,n,p", [(6144, 300, 40), (6145, 300, 40), (8193, 255, 16), (8193, 256, 16), (6100, 100_000, 33), (30_000, 70_000, 24), (100_001, 1, 65),
                                        (50_000, 3, 128), (40_000, 600, 7), (5000, 1, 512), (70_000, 20, 1000)])
 def test_gradient_of_ids_that_occur_often(B, count, n, p, weighted):
     gen = _gen(count + n)
@@ -256,6 +257,23 @@ def test_offsets_beyond_32_bits(B):
     assert torch.equal(de[n - 2], dy[2]) and torch.equal(de[0], dy[1]) and torch.equal(de[1_050_001], dy[5])
     assert torch.equal(de[n - 1], (dy[0].float() + dy[4].float()).bfloat16())
     assert int((de != 0).any(1).sum()) == 4
+
+
+@pytest.mark.parametrize("pad", [0, 4])
+@pytest.mark.parametrize("count", [100, 7000])
+def test_few_entries_of_a_large_matrix(B, count, pad):
+    """More than 256 MB with few rows of entries: cleared as a whole; what lies between the rows stays."""
+    n, p = 70_000, 1000
+    gen = _gen(count)
+    ids = _ids(count, n, gen)
+    dy, _ = V.matrix(count, p, torch.float32, gen)
+    de = torch.full((n, p + pad), 7.0, device="cuda")
+    B.spsyrk_lookup_grad(ids, dy, n, de=de[:, :p])
+    held = (ids >= 0) & (ids < n)
+    expected, size = (torch.zeros((n, p), dtype=torch.float64, device="cuda").index_add_(0, ids[held].long(), t[held]) for t in (dy.double(), dy.double().abs()))
+    often = torch.bincount(ids[held].long(), minlength=n)[:, None]
+    V.check(de[:, :p], expected, (often + 6) * 2.0 ** -24 * size + V.half_step(de.dtype, expected))
+    assert (de[:, p:] == 7).all()
 
 
 @pytest.mark.parametrize("count", [700, 9000])
