@@ -341,7 +341,7 @@ __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float wei
     if (c.lse) c.lse[row] = left_out ? 0.f : (float)((double)b * c.inv_tau_d + rest);
 }
 
-// What the CTAs of a cluster tell one another and the warps of a CTA theirs: running sums of the student's and of the teacher's row.
+// What the warps of a CTA tell one another: running sums of the student's and of the teacher's row.
 struct Joint {
     Running student, teacher;
 };
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
         for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {
             const int32_t id = s_id[t];
             if (id < 0 || !is_mine(id)) continue;
-            for (int q = (int)(((uint32_t)id * 2654435761u)   >> (32 - c.log_slots));; q = (q + 1) & (slots - 1)) {  // (multiplicative hashing; at most half full)
+            for (int q = (int)(((uint32_t)id * 2654435761u) >> (32 - c.log_slots));; q = (q + 1) & (slots - 1)) {  // (multiplicative hashing; at most half full)
                 const uint16_t was = atomicCAS(&table[q], NO_ENTRY, (uint16_t)t);
                 if (was == NO_ENTRY) {
                     chosen |= 1u << bit;
@@ -507,10 +507,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     }
     if (!few && FORWARD) {  // the loss needs logits that the gradient may overwrite
         if (rank == 0) write_loss<T, THREADS>(c, row, weight, e0, entries, false, s_id, s_z, s_at, s, r, top, teacher);
-        if (size > 1) {
-            cluster_arrive();
-            cluster_wait();
-        }
+        if (size > 1) cluster_sync();
     }
     if (teacher.sum == 0.f) {  // no entry with a logit other than -infinity
         leave_out();

@@ -116,15 +116,10 @@ struct Rows {
     }
 };
 
-// Thread-block clusters: this CTA's number, the number of CTAs, a barrier, and values in another CTA's shared memory.
+// Thread-block clusters: this CTA's number, a barrier, and values in another CTA's shared memory.
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
 // (relaxed: says only that this CTA has come so far, and that its barriers in shared memory, made visible, are there)
