@@ -493,7 +493,12 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     }
     // p_t = e_t * unit with e_t as in teacher.sum, mass P
     const float top = base_of(teacher.most);
-    const float unit = c.teacher.lse ? expf((float)(base_in_nats(top, c) - (double)c.teacher.lse[row])) : 1.f / teacher.sum;
+    float unit = 1.f / teacher.sum;
+    if (c.teacher.lse) {  // (the exponent in two parts: rounded as a whole, one of 40 is off by 2e-6)
+        const double x = base_in_nats(top, c) - (double)c.teacher.lse[row];
+        const float whole = (float)x, rest = isfinite(whole) ? (float)(x - (double)whole) : 0.f;
+        unit = expf(whole) * (1.f + rest);
+    }
     const float mass = c.teacher.lse ? teacher.sum * unit : 1.f + 0.f * teacher.sum;  // (1, or NaN)
     auto e_of = [&](float z) { return term(z, top, c.k); };
 

@@ -94,7 +94,7 @@ def test_ragged_rows_weights_and_a_given_norm(B, dtype, teacher_dtype):
     r = torch.randn(m, generator=gen, device="cuda")
     r[2] = r[7] = 0.0
     lse = torch.full((m,), 12.0, device="cuda") + torch.rand(m, generator=gen, device="cuda")
-    for kw in (dict(), dict(row_weights=r), dict(teacher_lse=lse), dict(row_weights=r, teacher_lse=lse, tau=1.7)):
+    for kw in (dict(), dict(row_weights=r), dict(teacher_lse=lse), dict(row_weights=r, teacher_lse=lse, tau=1.7), dict(teacher_lse=lse + 28.0, tau=0.5)):
         loss, norm, grad = _check(B, logits, ids, z, rowptr=rowptr, **kw)
         out = torch.tensor(lengths, device="cuda") == 0
         if "row_weights" in kw:

@@ -99,7 +99,8 @@ def distill_plain(logits, ids, teacher, rowptr, teacher_lse, row_weights, tau, s
     d_t = 2^-22 + 2^-23 a.  One of the student: 2^-22 (ex2.approx), its argument, b in units of ln 2, by the roundings of the
     factor and of the multiply-add, 2^-23 b ln 2.  Sum of a row: every thread adds up to c = n / 512 + 16 terms and corrects its sum
     at most as often (2^-22 and 2^-23 of the exponent each, below 2^-21 as long as the exponents of corrections sum to less than 2^10),
-    then 15 levels of joining: D = (2 c + 60) 2^-22 + the mean of the terms' own errors.
+    then 15 levels of joining: D = (2 c + 60) 2^-22 + the mean of the terms' own errors.  An exponential below 2^-126 is 0 (ex2.approx.ftz flushes what
+    would be subnormal): off by up to 2^-126, times the gradient's factor where that is not in the exponent already.
     """
     m, n = logits.shape
     nnz = ids.numel()
@@ -137,7 +138,7 @@ def distill_plain(logits, ids, teacher, rowptr, teacher_lse, row_weights, tau, s
         loss_b[i] = abs(scale * r) * (spread + mass * (total + 2.0 ** -22)) + 2.0 ** -23 * loss[i].abs()
         pd = (p * (2 * d + 2.0 ** -22)).sum()  # the norm takes part in the errors of all
         per_id = torch.zeros(n, dtype=torch.float64, device="cuda").scatter_add(0, at, p * (d + pd / max(mass, 1e-300) + 2.0 ** -22 + at.numel() * 2.0 ** -24))
-        grad_b[i] = (mass * q * (own + total + 2.0 ** -22 + 2.0 ** -23 * (1 + abs(float(lse[i]))) + pd) + per_id) * abs(scale * r / tau)
+        grad_b[i] = (mass * q * (own + total + 2.0 ** -22 + 2.0 ** -23 * (1 + abs(float(lse[i]))) + pd) + per_id) * abs(scale * r / tau) + 2.0 ** -126 * (1 + mass * abs(scale * r / tau))
     return (loss, lse, grad), (loss_b, lse_b, grad_b)
 
 
