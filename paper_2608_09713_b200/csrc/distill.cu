@@ -53,20 +53,28 @@ __device__ __forceinline__ float power_of_two(float v) {
 }
 
 // The sum of 2^(k s) over logits s, k = log2(e) / tau, as sum * 2^at: `most` is the largest logit so far (-infinity if there was
-// none) and at = most * k, rounded, is what the exponents are taken relative to: rounding it moves nothing, since the terms, the
-// changes of `most` and the logarithm at the end all use the same number.  Logits beyond LARGE, whose products could overflow (rows masked
-// with the lowest value throughout), go by (s - most) * k instead.
+// none) and `at` what the exponents are taken relative to.  As long as most * k is below NEAR in size, `at` is that product, rounded: a term is
+// one multiply-add, and rounding `at` moves nothing, since the terms, the changes of `most` and the logarithm at the end all use the
+// same number.  Half a step of a larger product would become an exponent of its own (2^7 at 1e9, infinity or 0 from 1.5e9 on): beyond NEAR
+// `at` is most * k itself and terms go by (s - most) * k.  slip() is what rounding has moved `at` by.
 struct Running {
     float most, sum;
 };
-constexpr float LARGE = 1e30f;
+constexpr float NEAR = 4096.f;
 __device__ __forceinline__ float base_of(float most) { return most == -CUDART_INF_F ? 0.f : most; }  // nothing but -infinity: terms of 0, or NaN
+__device__ __forceinline__ bool is_near(float most, float k) { return fabsf(__fmul_rn(most, k)) < NEAR; }
+__device__ __forceinline__ float slip(float most, float k) {
+    const float at = __fmul_rn(most, k);
+    return fabsf(at) < NEAR ? -fmaf(most, k, -at) : 0.f;
+}
 __device__ __forceinline__ float step_down(float from, float to, float k) {  // the factor when `most` goes from one to the other
-    if (fabsf(to) < LARGE && fabsf(from) < LARGE) return power_of_two(__fmul_rn(from, k) - __fmul_rn(to, k));
-    return power_of_two((from - to) * k);
+    const float a = __fmul_rn(from, k), b = __fmul_rn(to, k);
+    if (fabsf(a) < NEAR && fabsf(b) < NEAR) return power_of_two(a - b);
+    return power_of_two((from - to) * k + (slip(from, k) - slip(to, k)));
 }
 __device__ __forceinline__ float term(float s, float base, float k) {
-    return power_of_two(fabsf(base) < LARGE ? fmaf(s, k, -__fmul_rn(base, k)) : (s - base) * k);
+    const float at = __fmul_rn(base, k);
+    return power_of_two(fabsf(at) < NEAR ? fmaf(s, k, -at) : (s - base) * k);
 }
 template <int N>
 __device__ __forceinline__ void take(Running& r, const float (&s)[N], float k) {
@@ -210,7 +218,7 @@ __device__ __forceinline__ void take_units(Running& r, const uint4 (&u)[U], floa
         r.most = top;
     }
     const float b = base_of(r.most), at = __fmul_rn(b, k);
-    if (fabsf(b) < LARGE) {
+    if (fabsf(at) < NEAR) {
         const Pair kk = pair(k, k), off = pair(-at, -at);
         Pair sum[2] = {pair(r.sum, 0.f), pair(0.f, 0.f)};
 #pragma unroll
@@ -270,12 +278,14 @@ struct Call {
 // What the terms of a running sum are taken relative to, as a logarithm.  (k is rounded, 1 / tau is not: base / tau, and what rounding
 // the product base k moved it by.)
 __device__ __forceinline__ double base_in_nats(float base, const Call& c) {
-    return (double)base * c.inv_tau_d + (fabsf(base) < LARGE ? ((double)__fmul_rn(base, c.k) - (double)base * (double)c.k) * LN2 : 0.0);
+    return (double)base * c.inv_tau_d + (double)slip(base, c.k) * LN2;
 }
 
 // The gradient of `left` units from `at` on (this thread's: every THREADS-th), but for the teacher's ids: a 2^(s k - shift).  FOLDED: the factor
 // is in the shift already (16-bit results: the approximate logarithm, off by 2^-22, and the shift's rounding are far below their steps).
-template <typename T, int THREADS, bool FOLDED>
+// BY_BASE: a 2^((s - shift) k).
+enum Form { FOLDED, BY_SHIFT, BY_BASE };
+template <typename T, int THREADS, Form FORM>
 __device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left, float k, float shift, float a) {
     constexpr int U = 4, PAIRS = Unit<T>::PAIRS;
     const Pair kk = pair(k, k), off = pair(-shift, -shift), aa = pair(a, a);
@@ -283,9 +293,10 @@ __device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left
         float2 y[PAIRS];
 #pragma unroll
         for (int q = 0; q < PAIRS; ++q) {
-            const float2 p = halves(multiply_add(Unit<T>::get(x, q), kk, off));
+            const Pair s = Unit<T>::get(x, q);
+            const float2 p = halves(FORM == BY_BASE ? multiply(add(s, off), kk) : multiply_add(s, kk, off));
             y[q] = float2{power_of_two(p.x), power_of_two(p.y)};
-            if (!FOLDED) y[q] = halves(multiply(pair(y[q].x, y[q].y), aa));
+            if (FORM != FOLDED) y[q] = halves(multiply(pair(y[q].x, y[q].y), aa));
         }
         return Unit<T>::put(y);
     };
@@ -526,15 +537,15 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
         float a, shift, b = 0.f;
         if (FORWARD) {
             b = base_of(r.most);
-            shift = fabsf(b) < LARGE ? __fmul_rn(b, c.k) : 0.f;
+            shift = is_near(b, c.k) ? __fmul_rn(b, c.k) : 0.f;
             a = r.sum > 0.f && r.sum < CUDART_INF_F ? factor * mass / r.sum : CUDART_NAN_F;
         } else {
             const double lse = (double)c.kept[row], exact = lse / c.inv_tau_d * (double)c.k;
             shift = (float)exact;
             const double slip = ((double)shift - exact) * LN2;
-            a = fabs(lse) < (double)LARGE ? (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip)) : CUDART_NAN_F;
+            a = fabs(lse) < 1e30 ? (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip)) : CUDART_NAN_F;
         }
-        const bool plain = fabsf(b) < LARGE;
+        const bool plain = !FORWARD || is_near(b, c.k);
         auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
         if (few) {
             const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
@@ -542,10 +553,11 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             const bool folded = sizeof(T) == 2 && plain && a > 0x1p-100f && a < 0x1p100f;
             const float deep = folded ? shift - __log2f(a) : shift;
             auto g_of = [&](float x) { return folded ? power_of_two(fmaf(x, c.k, -deep)) : a * q_of(x); };  // the same wherever the rows lie
-            if (plain && aligned) {
+            if (aligned) {
                 uint4* to = reinterpret_cast<uint4*>(g + mine.first) + tid;
-                if (folded) write_units<T, THREADS, true>(at, to, left, c.k, deep, a);
-                else write_units<T, THREADS, false>(at, to, left, c.k, shift, a);
+                if (folded) write_units<T, THREADS, FOLDED>(at, to, left, c.k, deep, a);
+                else if (plain) write_units<T, THREADS, BY_SHIFT>(at, to, left, c.k, shift, a);
+                else write_units<T, THREADS, BY_BASE>(at, to, left, c.k, b, a);
             } else {
                 T* const to = g + mine.first;
                 for (int u = tid; u < left; u += THREADS, at += THREADS) {
