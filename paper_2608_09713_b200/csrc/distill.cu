@@ -282,7 +282,8 @@ __device__ __forceinline__ double base_in_nats(float base, const Call& c) {
 }
 
 // The gradient of `left` units from `at` on (this thread's: every THREADS-th), but for the teacher's ids: a 2^(s k - shift).  FOLDED: the factor
-// is in the shift already (16-bit results: the approximate logarithm, off by 2^-22, and the shift's rounding are far below their steps).
+// is in the shift already (16-bit results whose shift and factor's logarithm are below 400 and 100 in size: half a step of their sum
+// is 2^-16 then, the approximate logarithm is off by 2^-22, and half a step of the result is 2^-12 of it or more).
 // BY_BASE: a 2^((s - shift) k).
 enum Form { FOLDED, BY_SHIFT, BY_BASE };
 template <typename T, int THREADS, Form FORM>
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
         if (few) {
             const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
             int left = mine.units;
-            const bool folded = sizeof(T) == 2 && plain && a > 0x1p-100f && a < 0x1p100f;
+            const bool folded = sizeof(T) == 2 && plain && fabsf(shift) < 400.f && a > 0x1p-100f && a < 0x1p100f;
             const float deep = folded ? shift - __log2f(a) : shift;
             auto g_of = [&](float x) { return folded ? power_of_two(fmaf(x, c.k, -deep)) : a * q_of(x); };  // the same wherever the rows lie
             if (aligned) {

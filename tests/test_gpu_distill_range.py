@@ -120,3 +120,39 @@ def test_a_given_norm_far_from_zero(B, base):
     loss, norm, grad = B.spsyrk_distill(logits, ids, z, teacher_lse=lse, grad=True)
     for got, e, b in zip((loss, norm, grad), expected, bounds):
         _check(got, e, b)
+
+
+# Where the gradient's factor goes into the exponent, the sum of the two is rounded once more: exponents below 2^9, half a step 2^-16, of the
+# student's part.
+@pytest.mark.parametrize("n,k", SIZES)
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16))
+@pytest.mark.parametrize("base", BASES)
+def test_half_precision_gradient_of_rows_far_from_zero(B, base, dtype, n, k):
+    if not _fits(base, dtype):
+        base = math.copysign(4e4, base)
+    logits, ids, z = _rows(base, dtype, n, k)
+    expected, bounds, student = _expected(logits, ids, z, 1.0, 1.0)
+    grad = B.spsyrk_distill(logits, ids, z, grad=True)[2]
+    _check(grad, expected[2], bounds[2] + 2.0 ** -16 * student)
+    B.spsyrk_distill(logits, ids, z, grad=logits)
+    assert torch.equal(logits, grad)
+
+
+@pytest.mark.parametrize("n,k", SIZES)
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16))
+@pytest.mark.parametrize("tau,base,spread", TEMPERATURES)
+def test_half_precision_gradient_at_temperatures(B, tau, base, spread, dtype, n, k):
+    logits, ids, z = _rows(base, dtype, n, k, spread)
+    expected, bounds, student = _expected(logits, ids, z, tau, tau)
+    grad = B.spsyrk_distill(logits, ids, z, temperature=tau, scale=tau, grad=True)[2]
+    _check(grad, expected[2], bounds[2] + 2.0 ** -16 * student)
+
+
+def test_half_precision_gradient_between_other_boundaries(B):
+    """A gradient whose rows lie otherwise than the logits goes element by element."""
+    for base in (2839.0, 4e4):
+        logits, ids, z = _rows(base, torch.float16, 333, 5)
+        expected, bounds, student = _expected(logits, ids, z, 1.0, 1.0)
+        room = torch.zeros(16 * 335 + 3, dtype=torch.float16, device="cuda")
+        grad = B.spsyrk_distill(logits, ids, z, grad=room[3:].view(16, 335)[:, :333])[2]
+        _check(grad, expected[2], bounds[2] + 2.0 ** -16 * student)
