@@ -462,8 +462,9 @@ spsyrk_status_t spsyrk_distill(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t
 /*
  * spsyrk_distill_grad - G of spsyrk_distill from the lse that a call without G has returned: the backward pass when the rows'
  * weights (the gradient of the losses times the weights of the forward pass) come later.  A row that was left out there must be
- * left out here.  (Logits that are all beyond 1e30 in size, as in a row that is masked throughout with the type's lowest value, leave no
- * room in lse for the rest of the sum: such a row's gradient is NaN here.)  Other arguments as there.
+ * left out here.  Where the lse is 1024 or more in size, which as a float leaves too little room for the rest of the sum (rows masked throughout
+ * with a large number), the sum is taken from the logits again; an lse that is NaN makes the row's gradient NaN.
+ * Other arguments as there.
  */
 spsyrk_status_t spsyrk_distill_grad(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t teacher_dtype,
                                     const int64_t *d_rowptr, const int32_t *d_ids, const void *d_teacher, const float *d_teacher_lse,

@@ -61,6 +61,8 @@ struct Running {
     float most, sum;
 };
 constexpr float NEAR = 4096.f;
+// A log sum of this size or more is too coarse as a float (half a step 2^-14): what is made from it is made from the logits again.
+constexpr float COARSE = 1024.f;
 __device__ __forceinline__ float base_of(float most) { return most == -CUDART_INF_F ? 0.f : most; }  // nothing but -infinity: terms of 0, or NaN
 __device__ __forceinline__ bool is_near(float most, float k) { return fabsf(__fmul_rn(most, k)) < NEAR; }
 __device__ __forceinline__ float slip(float most, float k) {
@@ -245,8 +247,7 @@ __device__ __forceinline__ void prefetch(const void* from, int bytes) {
 // A row's columns in 16-byte units from its first 16-byte boundary: this CTA has `units` of them from column `first` on, and the
 // first CTA also the `head` columns before the boundary and those from `tail` on, behind the last unit.
 struct Share {
-    int head, units;
-    int64_t first, tail;
+    int head, units, first, tail;
 };
 template <typename T>
 __device__ __forceinline__ Share share_of(const T* row, int64_t n, uint32_t rank, int log_size) {
@@ -255,8 +256,8 @@ __device__ __forceinline__ Share share_of(const T* row, int64_t n, uint32_t rank
     s.head = (int)min(n, (int64_t)((0 - reinterpret_cast<uintptr_t>(row)) % 16 / sizeof(T)));
     const int units = (int)((uint32_t)(n - s.head) / W), each = (units + (1 << log_size) - 1) >> log_size, v0 = min(units, (int)rank * each);
     s.units = min(units - v0, each);
-    s.first = s.head + (int64_t)v0 * W;
-    s.tail = s.head + (int64_t)units * W;
+    s.first = s.head + v0 * W;
+    s.tail = s.head + units * W;
     return s;
 }
 
@@ -358,7 +359,7 @@ struct Joint {
     Running student, teacher;
 };
 
-// FORWARD: the sum over the row is computed (else it is `kept`); GRAD: the gradient is written.
+// FORWARD: the sum over the row is computed (else it is `kept`, unless that is too coarse); GRAD: the gradient is written.
 template <typename T, int THREADS, bool FORWARD, bool GRAD>
 __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_kernel(const Call c, const T* logits, T* grad) {
     constexpr int W = 16 / (int)sizeof(T), U = 4, WARPS = THREADS / 32;
@@ -381,8 +382,8 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     const bool few = entries <= c.top;
     const Share mine = share_of(s, c.n, rank, c.log_cluster);
     const bool aligned = !GRAD || reinterpret_cast<uintptr_t>(g + mine.head) % 16 == 0;
-    const int64_t last = mine.first + (int64_t)mine.units * W;
-    auto is_mine = [&](int64_t id) { return (id >= mine.first && id < last) || (rank == 0 && (id < mine.head || id >= mine.tail)); };
+    const int last = mine.first + mine.units * W, behind = (int)c.n - mine.tail;  // (columns behind the last unit)
+    auto is_mine = [&](int id) { return (id >= mine.first && id < last) || (rank == 0 && (id < mine.head || id >= mine.tail)); };
 
     auto leave_out = [&] {  // (the same for the whole cluster)
         if (FORWARD && tid == 0 && rank == 0) {
@@ -393,11 +394,11 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             if (aligned) {
                 for (int u = tid; u < mine.units; u += THREADS) *reinterpret_cast<uint4*>(g + mine.first + (int64_t)u * W) = uint4{0, 0, 0, 0};
             } else {
-                for (int64_t v = mine.first + tid; v < last; v += THREADS) g[v] = narrow<T>(0.f);
+                for (int v = tid; v < last - mine.first; v += THREADS) g[mine.first + v] = narrow<T>(0.f);
             }
             if (rank == 0) {
                 if (tid < mine.head) g[tid] = narrow<T>(0.f);
-                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(0.f);
+                if (tid < behind) g[mine.tail + tid] = narrow<T>(0.f);
             }
         }
     };
@@ -437,6 +438,8 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     }
 
     Running r{-CUDART_INF_F, 0.f};
+    const float kept = FORWARD ? 0.f : c.kept[row];
+    const bool sums = FORWARD || fabsf(kept) >= COARSE;  // the row's sum is computed
     if (FORWARD) {
         const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
         int left = mine.units;
@@ -456,25 +459,32 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             }
             take_units<T, U>(r, x, c.k);
         }
+    } else if (sums) {
+        for (int u = tid; u < mine.units; u += THREADS) {
+            const uint4 x[1] = {__ldcg(reinterpret_cast<const uint4*>(s + mine.first) + u)};
+            take_units<T, 1>(r, x, c.k);
+        }
+    }
+    if (sums) {
         if (rank == 0) {
             float f[1];
             if (tid < mine.head) {
                 f[0] = widen(s[tid]);
                 take<1>(r, f, c.k);
             }
-            if (mine.tail + tid < c.n) {
+            if (tid < behind) {
                 f[0] = widen(s[mine.tail + tid]);
                 take<1>(r, f, c.k);
             }
         }
     }
     // joined over the warp, the CTA, the cluster
-    if (FORWARD) r = join<32>(r, c.k);
+    if (sums) r = join<32>(r, c.k);
     if ((tid & ~31) < entries) teacher = join<32>(teacher, c.k);
     if (lane_id() == 0) s_warp[tid >> 5] = Joint{r, teacher};
     __syncthreads();
     const Joint joint = s_warp[lane_id() & (WARPS - 1)];
-    if (FORWARD) r = join<WARPS>(joint.student, c.k);
+    if (sums) r = join<WARPS>(joint.student, c.k);
     teacher = join<WARPS>(joint.teacher, c.k);
     if (size > 1) {
         cluster_wait();
@@ -516,7 +526,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
 
     if (size > 1) {
         const bool all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
-        if (FORWARD) {
+        if (sums) {
             const float2 part = s_cta[lane_id() & (size - 1)];
             r = Running{part.x, all ? part.y : CUDART_NAN_F};  // (a wait that runs out, which should not happen, is seen in the results)
             r = size == 2 ? join<2>(r, c.k) : size == 4 ? join<4>(r, c.k) : join<8>(r, c.k);
@@ -533,20 +543,20 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     if (GRAD) {
         // G_v = a 2^(s k - shift) - (at the teacher's ids) f e; a row that was NaN or -infinity throughout is NaN in all places.  The shift that
         // belongs to a kept lse is that of a logit with q = 1, so that the rounding of k matters to small q only; what
-        // rounding the shift takes away goes into a (its logarithm is below 2^-15: two terms of the exponential's series are exact to 2^-45).
+        // rounding the shift takes away goes into a (its logarithm is below 2^-14: two terms of the exponential's series are exact to 2^-44).
         const float factor = c.factor * weight, f = factor * unit;
         float a, shift, b = 0.f;
-        if (FORWARD) {
+        if (sums) {
             b = base_of(r.most);
             shift = is_near(b, c.k) ? __fmul_rn(b, c.k) : 0.f;
             a = r.sum > 0.f && r.sum < CUDART_INF_F ? factor * mass / r.sum : CUDART_NAN_F;
         } else {
-            const double lse = (double)c.kept[row], exact = lse / c.inv_tau_d * (double)c.k;
+            const double exact = (double)kept / c.inv_tau_d * (double)c.k;
             shift = (float)exact;
             const double slip = ((double)shift - exact) * LN2;
-            a = fabs(lse) < 1e30 ? (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip)) : CUDART_NAN_F;
+            a = (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip));
         }
-        const bool plain = !FORWARD || is_near(b, c.k);
+        const bool plain = !sums || is_near(b, c.k);
         auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
         if (few) {
             const uint4* at = reinterpret_cast<const uint4*>(s + mine.first) + tid;
@@ -570,7 +580,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             }
             if (rank == 0) {
                 if (tid < mine.head) g[tid] = narrow<T>(g_of(widen(s[tid])));
-                if (mine.tail + tid < c.n) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
+                if (tid < behind) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
             }
             __syncthreads();
             for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {

@@ -156,3 +156,43 @@ def test_half_precision_gradient_between_other_boundaries(B):
         room = torch.zeros(16 * 335 + 3, dtype=torch.float16, device="cuda")
         grad = B.spsyrk_distill(logits, ids, z, grad=room[3:].view(16, 335)[:, :333])[2]
         _check(grad, expected[2], bounds[2] + 2.0 ** -16 * student)
+
+
+# The gradient from a kept lse: a float below 2^10 is off by 2^-24 of itself; of a larger one nothing is asked.
+def _check_kept(B, logits, ids, z, tau):
+    expected, bounds, student = _expected(logits, ids, z, tau, tau)
+    bound = bounds[2] + (2.0 ** -16 + 2.0 ** -24 * expected[1].abs().clamp(max=1024.0)[:, None]) * student
+    lse = B.spsyrk_distill(logits, ids, z, temperature=tau, scale=tau)[1]
+    grad = B.spsyrk_distill_grad(logits, lse, ids, z, temperature=tau, scale=tau)
+    _check(grad, expected[2], bound)
+    B.spsyrk_distill_grad(logits, lse, ids, z, temperature=tau, scale=tau, grad=logits)
+    assert torch.equal(logits, grad)
+
+
+@pytest.mark.parametrize("n,k", SIZES)
+@pytest.mark.parametrize("dtype", LOGITS)
+@pytest.mark.parametrize("base", BASES + (1000.0, 1020.0, 1030.0, -1015.0, -1030.0))
+def test_gradient_from_a_kept_lse_of_rows_far_from_zero(B, base, dtype, n, k):
+    if not _fits(base, dtype):
+        base = math.copysign(4e4, base)
+    _check_kept(B, *_rows(base, dtype, n, k), 1.0)
+
+
+@pytest.mark.parametrize("n,k", SIZES)
+@pytest.mark.parametrize("dtype", LOGITS)
+@pytest.mark.parametrize("tau,base,spread", TEMPERATURES)
+def test_gradient_from_a_kept_lse_at_temperatures(B, tau, base, spread, dtype, n, k):
+    _check_kept(B, *_rows(base, dtype, n, k, spread), tau)
+
+
+@pytest.mark.parametrize("n", [500, 50_000])
+def test_gradient_from_a_kept_lse_of_rows_that_are_nan(B, n):
+    """Rows with NaN or infinity, and rows whose lse is one; their neighbours are not touched by it."""
+    logits = torch.randn((6, n), generator=_gen(n), device="cuda") * 2000
+    ids = torch.zeros((6, 1), dtype=torch.int32, device="cuda")
+    z = torch.zeros((6, 1), device="cuda")
+    logits[0, 3], logits[1, 3], logits[2] = math.nan, math.inf, -math.inf
+    lse = B.spsyrk_distill(logits, ids, z)[1]
+    lse[4] = math.nan
+    grad = B.spsyrk_distill_grad(logits, lse, ids, z)
+    assert grad[[0, 1, 2, 4]].isnan().all() and not grad[[3, 5]].isnan().any()
