@@ -69,34 +69,39 @@ __device__ __forceinline__ float slip(float most, float k) {
     const float at = __fmul_rn(most, k);
     return fabsf(at) < NEAR ? -fmaf(most, k, -at) : 0.f;
 }
+// (ALWAYS: a sum of few terms, the teacher's, whose exponents go by the difference whatever their size.)
+template <bool ALWAYS = false>
 __device__ __forceinline__ float step_down(float from, float to, float k) {  // the factor when `most` goes from one to the other
+    if (ALWAYS) return power_of_two((from - to) * k);
     const float a = __fmul_rn(from, k), b = __fmul_rn(to, k);
     if (fabsf(a) < NEAR && fabsf(b) < NEAR) return power_of_two(a - b);
     return power_of_two((from - to) * k + (slip(from, k) - slip(to, k)));
 }
+template <bool ALWAYS = false>
 __device__ __forceinline__ float term(float s, float base, float k) {
+    if (ALWAYS) return power_of_two((s - base) * k);
     const float at = __fmul_rn(base, k);
     return power_of_two(fabsf(at) < NEAR ? fmaf(s, k, -at) : (s - base) * k);
 }
-template <int N>
+template <int N, bool ALWAYS = false>
 __device__ __forceinline__ void take(Running& r, const float (&s)[N], float k) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, s[i]);
     if (top > r.most) {
-        r.sum *= step_down(r.most, top, k);  // most = -infinity: times 0
+        r.sum *= step_down<ALWAYS>(r.most, top, k);  // most = -infinity: times 0
         r.most = top;
     }
     const float b = base_of(r.most);
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.sum += term(s[i], b, k);
+    for (int i = 0; i < N; ++i) r.sum += term<ALWAYS>(s[i], b, k);
 }
 // Running sums of N lanes (a power of two, the same ones in all groups of N) joined; all lanes get the same bits.
-template <int N>
+template <int N, bool ALWAYS = false>
 __device__ __forceinline__ Running join(Running r, float k) {
     float top;
     asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(r.most));
-    r.sum *= step_down(r.most, base_of(top), k);  // (0 times 0 for a lane that has nothing; NaN stays NaN)
+    r.sum *= step_down<ALWAYS>(r.most, base_of(top), k);  // (0 times 0 for a lane that has nothing; NaN stays NaN)
 #pragma unroll
     for (int o = N / 2; o > 0; o >>= 1) r.sum += __shfl_xor_sync(FULL_MASK, r.sum, o);
     return Running{top, r.sum};
@@ -276,12 +281,6 @@ struct Call {
     int top, log_slots; // entries that are kept in shared memory; slots of the hash table, at least twice as many
 };
 
-// What the terms of a running sum are taken relative to, as a logarithm.  (k is rounded, 1 / tau is not: base / tau, and what rounding
-// the product base k moved it by.)
-__device__ __forceinline__ double base_in_nats(float base, const Call& c) {
-    return (double)base * c.inv_tau_d + (double)slip(base, c.k) * LN2;
-}
-
 // The gradient of `left` units from `at` on (this thread's: every THREADS-th), but for the teacher's ids: a 2^(s k - shift).  FOLDED: the factor
 // is in the shift already (16-bit results whose shift and factor's logarithm are below 400 and 100 in size: half a step of their sum
 // is 2^-16 then, the approximate logarithm is off by 2^-22, and half a step of the result is 2^-12 of it or more).
@@ -324,7 +323,7 @@ __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float wei
         const int32_t id = few ? s_id[t] : c.teacher.ids[e0 + t];
         if (id < 0 || id >= c.n) continue;
         const float z = few ? s_z[t] : c.teacher.logit(e0 + t), at = few ? s_at[t] : widen(s[id]);
-        const float e = term(z, top, c.k);
+        const float e = term<true>(z, top, c.k);
         if (e == 0.f) continue;
         mass += (double)e;
         cross += (double)e * (((double)z - (double)top) - ((double)at - (double)b));
@@ -344,13 +343,12 @@ __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float wei
         mass += s_sum[w][0];
         cross += s_sum[w][1];
     }
-    // log p = (z - top) / tau + log_unit - slip, log q = (s - b) / tau - rest; p = e * unit
-    const double slip_of_top = base_in_nats(top, c) - (double)top * c.inv_tau_d;
-    const double rest = base_in_nats(b, c) - (double)b * c.inv_tau_d + log((double)r.sum);
-    const double log_unit = c.teacher.lse ? base_in_nats(top, c) - (double)c.teacher.lse[row] : -log(mass);
+    // log p = (z - top) / tau + log_unit, log q = (s - b) / tau - rest; p = e * unit.  (k is rounded, 1 / tau is not: it stands for differences only.)
+    const double rest = (double)slip(b, c.k) * LN2 + log((double)r.sum);
+    const double log_unit = c.teacher.lse ? (double)top * c.inv_tau_d - (double)c.teacher.lse[row] : -log(mass);
     const double unit = c.teacher.lse ? exp(log_unit) : 1.0 / mass;
     const bool left_out = teacher.sum == 0.f;
-    if (c.loss) c.loss[row] = left_out ? 0.f : (float)(c.scale * (double)weight * unit * (cross * c.inv_tau_d + mass * (log_unit - slip_of_top + rest)));
+    if (c.loss) c.loss[row] = left_out ? 0.f : (float)(c.scale * (double)weight * unit * (cross * c.inv_tau_d + mass * (log_unit + rest)));
     if (c.lse) c.lse[row] = left_out ? 0.f : (float)((double)b * c.inv_tau_d + rest);
 }
 
@@ -428,7 +426,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             s_z[t] = z[0];
             s_at[t] = held && (rank == 0 || is_mine(id)) ? widen(s[id]) : 0.f;
         }
-        take<1>(teacher, z, c.k);
+        take<1, true>(teacher, z, c.k);
     }
     const int slots = 1 << c.log_slots;
     constexpr uint16_t NO_ENTRY = 0xffff;
@@ -480,12 +478,12 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     }
     // joined over the warp, the CTA, the cluster
     if (sums) r = join<32>(r, c.k);
-    if ((tid & ~31) < entries) teacher = join<32>(teacher, c.k);
+    if ((tid & ~31) < entries) teacher = join<32, true>(teacher, c.k);
     if (lane_id() == 0) s_warp[tid >> 5] = Joint{r, teacher};
     __syncthreads();
     const Joint joint = s_warp[lane_id() & (WARPS - 1)];
     if (sums) r = join<WARPS>(joint.student, c.k);
-    teacher = join<WARPS>(joint.teacher, c.k);
+    teacher = join<WARPS, true>(joint.teacher, c.k);
     if (size > 1) {
         cluster_wait();
         if (tid == 0) barrier_expect(&s_arrived, size * 8);
@@ -517,12 +515,12 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     const float top = base_of(teacher.most);
     float unit = 1.f / teacher.sum;
     if (c.teacher.lse) {  // (the exponent in two parts: rounded as a whole, one of 40 is off by 2e-6)
-        const double x = base_in_nats(top, c) - (double)c.teacher.lse[row];
+        const double x = (double)top * c.inv_tau_d - (double)c.teacher.lse[row];
         const float whole = (float)x, rest = isfinite(whole) ? (float)(x - (double)whole) : 0.f;
         unit = expf(whole) * (1.f + rest);
     }
     const float mass = c.teacher.lse ? teacher.sum * unit : 1.f + 0.f * teacher.sum;  // (1, or NaN)
-    auto e_of = [&](float z) { return term(z, top, c.k); };
+    auto e_of = [&](float z) { return term<true>(z, top, c.k); };
 
     if (size > 1) {
         const bool all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
@@ -564,6 +562,12 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             const bool folded = sizeof(T) == 2 && plain && fabsf(shift) < 400.f && a > 0x1p-100f && a < 0x1p100f;
             const float deep = folded ? shift - __log2f(a) : shift;
             auto g_of = [&](float x) { return folded ? power_of_two(fmaf(x, c.k, -deep)) : a * q_of(x); };  // the same wherever the rows lie
+            auto write_ends = [&] {
+                if (rank != 0) return;
+                if (tid < mine.head) g[tid] = narrow<T>(g_of(widen(s[tid])));
+                if (tid < behind) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
+            };
+            if (!FORWARD) write_ends();  // (before or after: what keeps registers from being spilled in the loops; 1999 rows of 50021 59 us against 65)
             if (aligned) {
                 uint4* to = reinterpret_cast<uint4*>(g + mine.first) + tid;
                 if (folded) write_units<T, THREADS, FOLDED>(at, to, left, c.k, deep, a);
@@ -578,10 +582,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
                     for (int q = 0; q < W; ++q) to[(int64_t)u * W + q] = narrow<T>(g_of(widen(x.x[q])));
                 }
             }
-            if (rank == 0) {
-                if (tid < mine.head) g[tid] = narrow<T>(g_of(widen(s[tid])));
-                if (tid < behind) g[mine.tail + tid] = narrow<T>(g_of(widen(s[mine.tail + tid])));
-            }
+            if (FORWARD) write_ends();
             __syncthreads();
             for (int t = tid, bit = 0; t < count; t += THREADS, ++bit) {
                 if (!(chosen >> bit & 1u)) continue;
