@@ -522,11 +522,12 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     const float mass = c.teacher.lse ? teacher.sum * unit : 1.f + 0.f * teacher.sum;  // (1, or NaN)
     auto e_of = [&](float z) { return term<true>(z, top, c.k); };
 
+    bool all = true;  // a wait that runs out, which should not happen, is seen in the results: NaN
     if (size > 1) {
-        const bool all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
+        all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
         if (sums) {
             const float2 part = s_cta[lane_id() & (size - 1)];
-            r = Running{part.x, all ? part.y : CUDART_NAN_F};  // (a wait that runs out, which should not happen, is seen in the results)
+            r = Running{part.x, all ? part.y : CUDART_NAN_F};
             r = size == 2 ? join<2>(r, c.k) : size == 4 ? join<4>(r, c.k) : join<8>(r, c.k);
         }
     }
@@ -554,6 +555,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
             const double slip = ((double)shift - exact) * LN2;
             a = (float)((double)(factor * mass) * (1.0 + slip + 0.5 * slip * slip));
         }
+        if (!FORWARD && !all) a = CUDART_NAN_F;
         const bool plain = !sums || is_near(b, c.k);
         auto q_of = [&](float x) { return power_of_two(plain ? fmaf(x, c.k, -shift) : (x - b) * c.k); };
         if (few) {
