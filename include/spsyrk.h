@@ -419,6 +419,7 @@ spsyrk_status_t spsyrk_lookup(int64_t m, int64_t n, int64_t p, int64_t nnz, spsy
  *
  * Two-step use: d_workspace == NULL: *workspace_bytes receives the scratch size for (m, n, p, nnz, dtype) with and without row pointers
  * and weights; then the call, with a workspace of at least that size, 256-byte aligned, that no other work uses until this has ended.
+ * (Should one of the bounded waits between the CTAs of the sort run out, which should not happen, the sums are NaN.)
  * Errors also: WORKSPACE.
  */
 spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, int64_t nnz, spsyrk_dtype_t dtype, spsyrk_dtype_t g_dtype,

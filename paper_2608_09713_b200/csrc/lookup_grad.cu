@@ -9,6 +9,7 @@
 // add up pieces (or rank the ids, if they are few).
 // Bound by memory: dY is read once (a row of several ids once per id, through L2), dE written once.
 #include <algorithm>
+#include <math_constants.h>
 
 #include "element.cuh"
 #include "radix.cuh"
@@ -286,10 +287,11 @@ __device__ __forceinline__ void write_row(G* __restrict__ at, int64_t left, A sc
     store_narrow<G, V>(at, left, x);
 }
 
-// A group of lanes per piece and slab of columns.
+// A group of lanes per piece and slab of columns.  (After a wait among the radix passes that has run out, places of the order hold whatever the
+// workspace did: keys are tested anyway, and a row is cut to the last one.)
 // (Registers decide: eight sums a lane take four rows at a time and three CTAs per SM, fewer sums two and five; the others cost 5 to 15 %.)
 template <typename T, typename G, int V>
-__global__ void __launch_bounds__(THREADS, V == 8 ? 3 : 5) add_pieces_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key,
+__global__ void __launch_bounds__(THREADS, V == 8 ? 3 : 5) add_pieces_kernel(int64_t nnz, uint32_t last_row, int64_t n, int64_t p, const uint32_t* __restrict__ key,
                                                              const uint32_t* __restrict__ row, const typename Wide<T>::type* __restrict__ weight,
                                                              typename Wide<T>::type scale, const T* __restrict__ dy, int64_t lddy, G* __restrict__ de,
                                                              int64_t ldde, bool accumulate, typename Wide<T>::type* __restrict__ part, int piece,
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(THREADS, V == 8 ? 3 : 5) add_pieces_kernel(int
     };
     for (int64_t e = e0; e < e1; e += share) {
         const bool on = e + in_share < e1;
-        const uint32_t my_key = on ? key[e + in_share] : NO_KEY, my_row = on ? row[e + in_share] : 0u;
+        const uint32_t my_key = on ? key[e + in_share] : NO_KEY, my_row = on ? min(row[e + in_share], last_row) : 0u;
         const A my_w = on && weight ? weight[e + in_share] : A(1);
         const int count = (int)min((int64_t)share, e1 - e);
         for (int q = 0; q < count; q += U) {
@@ -427,10 +429,18 @@ struct Seams {
 
 template <typename A, typename G>
 __global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, int64_t p, const uint32_t* __restrict__ key, const A* __restrict__ part,
-                                                       A* __restrict__ part_out, A scale, G* __restrict__ de, int64_t ldde, bool accumulate, int64_t piece) {
+                                                       A* __restrict__ part_out, A scale, G* __restrict__ de, int64_t ldde, bool accumulate, int64_t piece,
+                                                       const uint32_t* __restrict__ err) {
     constexpr int N = JOIN_COLS / 32;
     __shared__ A left[THREADS / 32][2][JOIN_COLS];
-    link(key, part);
+    link(key, part, err);
+    if (err && *err) {  // a wait among the radix passes has run out, which should not happen: what the entries of this block name becomes NaN
+        const int64_t end = min(((int64_t)blockIdx.x + 1) * JOIN * piece, nnz);
+        for (int64_t e = (int64_t)blockIdx.x * JOIN * piece + (threadIdx.x >> 5); e < end; e += THREADS / 32)
+            for (int64_t c = (int64_t)blockIdx.y * JOIN_COLS + lane_id(); key[e] < (uint32_t)n && c < min(p, ((int64_t)blockIdx.y + 1) * JOIN_COLS); c += 32)
+                de[(int64_t)key[e] * ldde + c] = narrow<G>(A(CUDART_NAN_F));
+        return;
+    }
     const int lane = lane_id(), warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.y * JOIN_COLS + lane, first = (int64_t)blockIdx.x * JOIN + warp * JOIN_EACH;
     auto write = [&](uint32_t id, A(&x)[N]) {
@@ -468,7 +478,7 @@ __global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, i
 }
 
 template <typename T, typename G, int V>
-spsyrk_status_t add_typed(const GradWs& w, int which, const Fill& fill, int64_t n, int64_t p, int64_t nnz, bool weighted, double scale, const void* dy, int64_t lddy, void* de,
+spsyrk_status_t add_typed(const GradWs& w, int which, const uint32_t* err, const Fill& fill, int64_t m, int64_t n, int64_t p, int64_t nnz, bool weighted, double scale, const void* dy, int64_t lddy, void* de,
                           int64_t ldde, bool accumulate, cudaStream_t st) {
     using A = typename Wide<T>::type;
     int64_t piece = piece_of(nnz, p);
@@ -482,7 +492,7 @@ spsyrk_status_t add_typed(const GradWs& w, int which, const Fill& fill, int64_t 
     if (ctas + fill_ctas >= (int64_t(1) << 31)) return SPSYRK_ERR_OVERFLOW;
     const uint32_t* const key = w.key[which];
     const A* weight = weighted ? static_cast<const A*>(w.weight[which]) : nullptr;
-    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)(ctas + fill_ctas), THREADS, 0, st, nnz, n, p, key, w.row[which], weight, (A)scale,
+    SPSYRK_CUDA_TRY(launch_linked(add_pieces_kernel<T, G, V>, (unsigned)(ctas + fill_ctas), THREADS, 0, st, nnz, (uint32_t)(m - 1), n, p, key, w.row[which], weight, (A)scale,
                                   static_cast<const T*>(dy), lddy, static_cast<G*>(de), ldde, accumulate, static_cast<A*>(w.part[0]), (int)piece, shift, slabs, w.present, fill,
                                   (int)fill_ctas));
     for (int level = 0; pieces > 1; ++level) {
@@ -498,7 +508,7 @@ spsyrk_status_t add_typed(const GradWs& w, int which, const Fill& fill, int64_t 
         cfg.numAttrs = 1;
         A* const out = level + 1 < JOIN_LEVELS ? static_cast<A*>(w.part[level + 1]) : nullptr;  // (null where one block holds all: nothing leaves it)
         SPSYRK_CUDA_TRY(launch_kernel(cfg, join_kernel<A, G>, nnz, n, p, key, static_cast<const A*>(w.part[level]), out, (A)scale, static_cast<G*>(de), ldde,
-                                      accumulate, piece));
+                                      accumulate, piece, err));
         piece *= JOIN;
         pieces = blocks;
     }
@@ -588,7 +598,7 @@ extern "C" spsyrk_status_t spsyrk_lookup_grad(int64_t m, int64_t n, int64_t p, i
     const int of_dy = together(d_dy, lddy, size), of_de = together(d_de, ldde, g_size);
     const bool wide = of_dy == (int)(16 / size) && of_de == (int)(16 / g_size), two = of_dy >= 2 && of_de >= 2;
     const bool weighted = d_weights != nullptr;
-#define ADD(T, G, V) add_typed<T, G, V>(w, which, fill, n, p, nnz, weighted, scale, d_dy, lddy, d_de, ldde, accumulate != 0, st)
+#define ADD(T, G, V) add_typed<T, G, V>(w, which, nnz > FEW ? w.err : nullptr, fill, m, n, p, nnz, weighted, scale, d_dy, lddy, d_de, ldde, accumulate != 0, st)
     switch (dtype) {
         case SPSYRK_F64: return wide ? ADD(double, double, 2) : ADD(double, double, 1);
         case SPSYRK_F32: return wide ? ADD(float, float, 4) : two ? ADD(float, float, 2) : ADD(float, float, 1);
