@@ -348,7 +348,9 @@ __device__ __forceinline__ void write_loss(const Call& c, int64_t row, float wei
     const double log_unit = c.teacher.lse ? (double)top * c.inv_tau_d - (double)c.teacher.lse[row] : -log(mass);
     const double unit = c.teacher.lse ? exp(log_unit) : 1.0 / mass;
     const bool left_out = teacher.sum == 0.f;
-    if (c.loss) c.loss[row] = left_out ? 0.f : (float)(c.scale * (double)weight * unit * (cross * c.inv_tau_d + mass * (log_unit + rest)));
+    // (p = 0 throughout, under a given norm far above, adds nothing, whatever q is)
+    const bool nothing = left_out || (unit == 0.0 && mass < CUDART_INF && r.sum > 0.f && r.sum < CUDART_INF_F);
+    if (c.loss) c.loss[row] = nothing ? 0.f : (float)(c.scale * (double)weight * unit * (cross * c.inv_tau_d + mass * (log_unit + rest)));
     if (c.lse) c.lse[row] = left_out ? 0.f : (float)((double)b * c.inv_tau_d + rest);
 }
 

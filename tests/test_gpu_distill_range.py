@@ -196,3 +196,18 @@ def test_gradient_from_a_kept_lse_of_rows_that_are_nan(B, n):
     lse[4] = math.nan
     grad = B.spsyrk_distill_grad(logits, lse, ids, z)
     assert grad[[0, 1, 2, 4]].isnan().all() and not grad[[3, 5]].isnan().any()
+
+
+@pytest.mark.parametrize("norm", [800.0, 1e5, math.inf])
+def test_a_norm_that_leaves_the_teacher_nothing(B, norm):
+    """p = 0 for every entry: nothing is added, not for q = 0 either; NaN among the logits is NaN all the same."""
+    logits = torch.zeros((6, 40), device="cuda")
+    logits[1, 1] = -math.inf
+    logits[2, 7], logits[3] = math.nan, -math.inf
+    ids = torch.tensor([[1, 2]] * 6, dtype=torch.int32, device="cuda")
+    z = torch.zeros((6, 2), device="cuda")
+    z[4, 1] = math.nan
+    z[5] = -math.inf
+    loss, lse, grad = B.spsyrk_distill(logits, ids, z, teacher_lse=torch.full((6,), norm, device="cuda"), grad=True)
+    assert (loss[[0, 1, 5]] == 0).all() and (grad[[0, 1, 5]] == 0).all()
+    assert loss[2:5].isnan().all() and grad[2:5].isnan().all()
