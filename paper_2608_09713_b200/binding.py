@@ -24,7 +24,7 @@ if not os.path.exists(LIB_PATH):
 
 _lib = ctypes.CDLL(LIB_PATH)
 
-OK = 0
+OK, ERR_WORKSPACE = 0, 3
 F64, F32, I32, BF16, F16 = 0, 1, 2, 3, 4
 TRIL, FULL = 0, 1
 NCLASS = 8
@@ -654,6 +654,8 @@ def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None
         _in_use_on(stream, workspace)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError(f"{where}: the workspace must be contiguous uint8")
+    elif workspace.numel() == 0:  # (its null pointer would ask for the size)
+        raise SpsyrkError(ERR_WORKSPACE, where)
     sz = ctypes.c_size_t(workspace.numel())
     _call(_lib.spsyrk_lookup_grad, where, (ids, dy, rowptr, weights, de, workspace), stream, m, n, p, nnz, code, g_code, _ptr(rowptr), ids.data_ptr(),
           _ptr(weights), scale, dy.data_ptr(), lddy, de.data_ptr(), ldde, 1 if accumulate else 0, workspace.data_ptr(), ctypes.byref(sz))
