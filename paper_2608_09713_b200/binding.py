@@ -535,9 +535,14 @@ def spsyrk_jaccard(m, row_begin, rows, a_rowptr, c_rowptr, c_colidx, c_counts, o
 
 # ------------------------------------------------------------------------------------------
 # Rows of ids and dense matrices: lookups, their gradients, distillation.  The work goes to the tensors' device whatever the
-# current one is, to `stream` or to the current stream of that device.
+# current one is, to `stream` or to the current stream of that device.  Results have no graph of torch's autograd: a model that trains
+# calls the gradients itself (in an autograd function, for instance).  What a call writes into counts as changed in place, so that a
+# backward pass that has kept it raises an error instead of reading the new values.
 # ------------------------------------------------------------------------------------------
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (torch.cuda's functions take 7 us of a call's 15)
+
+
+_changed_in_place = torch.autograd.graph.increment_version
 
 
 def _call(fn, where, tensors, stream, *args):
@@ -606,7 +611,8 @@ def spsyrk_lookup(ids, e, rowptr=None, weights=None, scale=1.0, y=None, stream=N
     lde = _matrix(e, "spsyrk_lookup", "e")
     m, nnz = _entries("spsyrk_lookup", ids, rowptr, weights, (_weight_dtype(e.dtype),), "weights")
     n, p = e.shape
-    if y is None:
+    given = y is not None
+    if not given:
         y = e.new_empty((m, p))
         ldy = max(p, 1)
         _in_use_on(stream, y)
@@ -614,6 +620,8 @@ def spsyrk_lookup(ids, e, rowptr=None, weights=None, scale=1.0, y=None, stream=N
         ldy = _matrix(y, "spsyrk_lookup", "y", m, p, e.dtype)
     _call(_lib.spsyrk_lookup, "spsyrk_lookup", (ids, e, rowptr, weights, y), stream, m, n, p, nnz, _REAL_CODE[e.dtype], _ptr(rowptr), ids.data_ptr(),
           _ptr(weights), scale, e.data_ptr(), lde, y.data_ptr(), ldy)
+    if given:
+        _changed_in_place(y)
     return y
 
 
@@ -637,7 +645,8 @@ def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None
     m, nnz = _entries(where, ids, rowptr, weights, (_weight_dtype(dy.dtype),), "weights")
     lddy = _matrix(dy, where, "dy", m)
     p = dy.shape[1]
-    if de is None:
+    given = de is not None
+    if not given:
         if accumulate:
             raise ValueError(f"{where}: nothing to add to")
         dtype = dy.dtype if dtype is None else dtype
@@ -659,6 +668,8 @@ def spsyrk_lookup_grad(ids, dy, n, rowptr=None, weights=None, scale=1.0, de=None
     sz = ctypes.c_size_t(workspace.numel())
     _call(_lib.spsyrk_lookup_grad, where, (ids, dy, rowptr, weights, de, workspace), stream, m, n, p, nnz, code, g_code, _ptr(rowptr), ids.data_ptr(),
           _ptr(weights), scale, dy.data_ptr(), lddy, de.data_ptr(), ldde, 1 if accumulate else 0, workspace.data_ptr(), ctypes.byref(sz))
+    if given:
+        _changed_in_place(de)
     return de
 
 
@@ -666,7 +677,8 @@ def spsyrk_lookup_grad_weights(ids, e, dy, rowptr=None, scale=1.0, dw=None, stre
     """dw_t = scale * <E[id_t], dY[row of t]>, shaped as the ids: the gradient of the weights."""
     where = "spsyrk_lookup_grad_weights"
     lde = _matrix(e, where, "e")
-    if dw is None:
+    given = dw is not None
+    if not given:
         dw = e.new_empty(ids.shape, dtype=_weight_dtype(e.dtype))
         _in_use_on(stream, dw)
     m, nnz = _entries(where, ids, rowptr, dw, (_weight_dtype(e.dtype),), "dw")
@@ -674,6 +686,8 @@ def spsyrk_lookup_grad_weights(ids, e, dy, rowptr=None, scale=1.0, dw=None, stre
     lddy = _matrix(dy, where, "dy", m, p, e.dtype)
     _call(_lib.spsyrk_lookup_grad_weights, where, (ids, e, dy, rowptr, dw), stream, m, n, p, nnz, _REAL_CODE[e.dtype], _ptr(rowptr), ids.data_ptr(), scale,
           e.data_ptr(), lde, dy.data_ptr(), lddy, dw.data_ptr())
+    if given:
+        _changed_in_place(dw)
     return dw
 
 
@@ -714,7 +728,7 @@ def spsyrk_distill(logits, ids, teacher, rowptr=None, teacher_lse=None, row_weig
     m, nnz, ldl = _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights)
     loss, lse = logits.new_empty(m, dtype=torch.float32), logits.new_empty(m, dtype=torch.float32)
     _in_use_on(stream, loss, lse)
-    with_grad, ldg = grad is not None and grad is not False, 0
+    with_grad, given, ldg = grad is not None and grad is not False, torch.is_tensor(grad), 0
     if with_grad:
         grad, ldg = _gradient(where, logits, ldl, grad, stream)
     else:
@@ -722,6 +736,8 @@ def spsyrk_distill(logits, ids, teacher, rowptr=None, teacher_lse=None, row_weig
     _call(_lib.spsyrk_distill, where, (logits, ids, teacher, rowptr, teacher_lse, row_weights, grad), stream, m, logits.shape[1], nnz, _REAL_CODE[logits.dtype],
           _REAL_CODE[teacher.dtype], _ptr(rowptr), ids.data_ptr(), teacher.data_ptr(), _ptr(teacher_lse), _ptr(row_weights), temperature,
           temperature * temperature if scale is None else scale, logits.data_ptr(), ldl, loss.data_ptr(), lse.data_ptr(), _ptr(grad), ldg)
+    if given:
+        _changed_in_place(grad)
     return (loss, lse, grad) if with_grad else (loss, lse)
 
 
@@ -732,10 +748,13 @@ def spsyrk_distill_grad(logits, lse, ids, teacher, rowptr=None, teacher_lse=None
     m, nnz, ldl = _distill_args(where, logits, ids, teacher, rowptr, teacher_lse, row_weights)
     if lse.dtype != torch.float32 or lse.shape != (m,) or not lse.is_contiguous():
         raise ValueError(f"{where}: lse must be contiguous float32, one for each row")
+    given = torch.is_tensor(grad)
     grad, ldg = _gradient(where, logits, ldl, grad, stream)
     _call(_lib.spsyrk_distill_grad, where, (logits, lse, ids, teacher, rowptr, teacher_lse, row_weights, grad), stream, m, logits.shape[1], nnz,
           _REAL_CODE[logits.dtype], _REAL_CODE[teacher.dtype], _ptr(rowptr), ids.data_ptr(), teacher.data_ptr(), _ptr(teacher_lse), _ptr(row_weights),
           temperature, temperature * temperature if scale is None else scale, logits.data_ptr(), ldl, lse.data_ptr(), grad.data_ptr(), ldg)
+    if given:
+        _changed_in_place(grad)
     return grad
 
 

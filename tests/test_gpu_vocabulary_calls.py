@@ -1,4 +1,5 @@
-"""How the lookups and the distillation are called: workspaces of the caller's own."""
+"""How the lookups and the distillation are called: workspaces of the caller's own, and tensors that a graph of
+torch's autograd has kept."""
 import pytest
 import torch
 
@@ -24,3 +25,28 @@ def test_workspaces(B):
         with pytest.raises(B.SpsyrkError) as refused:
             B.spsyrk_lookup_grad(ids, dy, 9, workspace=room[:bytes])
         assert refused.value.status == 3
+
+
+def test_what_is_written_into_counts_as_changed(B):
+    """A backward pass that has kept a tensor before a call wrote into it raises an error; results have no graph."""
+    ids = torch.arange(4, dtype=torch.int32, device="cuda")
+    pairs, z = ids.view(4, 1), torch.zeros((4, 1), device="cuda")
+    fresh = lambda rows, cols=8: torch.randn((rows, cols), device="cuda", requires_grad=True) * 2.0
+    e, dy = torch.ones((9, 8), device="cuda"), torch.ones((4, 8), device="cuda")
+    lse = torch.zeros(4, device="cuda")
+    calls = [(fresh(4), lambda t: B.spsyrk_lookup(ids, e, y=t)), (fresh(9), lambda t: B.spsyrk_lookup_grad(ids, dy, 9, de=t)),
+             (fresh(9), lambda t: B.spsyrk_lookup_grad(ids, dy, 9, de=t, accumulate=True)),
+             (fresh(4, 1), lambda t: B.spsyrk_lookup_grad_weights(pairs, e, dy, dw=t)),
+             (fresh(4), lambda t: B.spsyrk_distill(t, pairs, z, grad=t)[2]), (fresh(4), lambda t: B.spsyrk_distill_grad(t, lse, pairs, z, grad=t))]
+    for kept, call in calls:
+        out = (kept * kept).sum()
+        assert call(kept) is kept
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            out.backward()
+    e = e.requires_grad_()
+    assert not B.spsyrk_lookup(ids, e).requires_grad
+    out = (e * e).sum()
+    B.spsyrk_lookup(ids, e)  # reads only
+    out.backward()
+    with torch.inference_mode():
+        assert torch.equal(B.spsyrk_lookup(ids, e, y=torch.empty((4, 8), device="cuda")), e[:4])
