@@ -539,9 +539,8 @@ def spsyrk_jaccard(m, row_begin, rows, a_rowptr, c_rowptr, c_colidx, c_counts, o
 # calls the gradients itself (in an autograd function, for instance).  What a call writes into counts as changed in place, so that a
 # backward pass that has kept it raises an error instead of reading the new values.
 # ------------------------------------------------------------------------------------------
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice  # (torch.cuda's functions take 7 us of a call's 15)
-
-
+# (torch.cuda's functions take 7 us of a call's 15; a torch without CUDA, whose tensors no call accepts, does not have these)
+_raw_stream, _current_device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
 _changed_in_place = torch.autograd.graph.increment_version
 
 
