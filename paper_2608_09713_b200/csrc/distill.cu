@@ -271,8 +271,8 @@ struct Call {
     int64_t n;
     Teacher teacher;
     const float* row_weights;
-    float k, inv_tau;   // log2(e) / tau, 1 / tau
-    double scale, inv_tau_d;
+    float k;                  // log2(e) / tau
+    double scale, inv_tau_d;  // 1 / tau
     int64_t ldl, ldg;
     float *loss, *lse;
     const float* kept;  // the rows' lse of an earlier call (gradient only)
@@ -693,7 +693,6 @@ spsyrk_status_t distill(int64_t m, int64_t n, int64_t nnz, spsyrk_dtype_t dtype,
     c.teacher = Teacher{d_ids, d_teacher, teacher_dtype, d_teacher_lse};
     c.row_weights = d_row_weights;
     c.k = (float)(LOG2E / temperature);
-    c.inv_tau = (float)(1.0 / temperature);
     c.inv_tau_d = 1.0 / temperature;
     c.scale = scale;
     c.factor = (float)(scale / temperature);
