@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(THREADS) read_ids_kernel(Rows a, int64_t n, co
                                                            unsigned long long* __restrict__ bins) {
     __shared__ int64_t span[2];
     __shared__ uint32_t h[RX_MAX_PASSES][RX_BINS];
-    __shared__ uint64_t marks[READ_MARKS];
+    __shared__ volatile uint64_t marks[READ_MARKS];  // (written by several threads at a time: one of their words, whole, is what volatile promises)
     for (int d = threadIdx.x; d < RX_MAX_PASSES * RX_BINS; d += THREADS) (&h[0][0])[d] = 0;
     for (int64_t base = (int64_t)blockIdx.x * READ_CHUNK; base < a.nnz; base += (int64_t)gridDim.x * READ_CHUNK) {
         __syncthreads();
