@@ -433,14 +433,7 @@ __global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, i
                                                        const uint32_t* __restrict__ err) {
     constexpr int N = JOIN_COLS / 32;
     __shared__ A left[THREADS / 32][2][JOIN_COLS];
-    link(key, part, err);
-    if (err && *err) {  // a wait among the radix passes has run out, which should not happen: what the entries of this block name becomes NaN
-        const int64_t end = min(((int64_t)blockIdx.x + 1) * JOIN * piece, nnz);
-        for (int64_t e = (int64_t)blockIdx.x * JOIN * piece + (threadIdx.x >> 5); e < end; e += THREADS / 32)
-            for (int64_t c = (int64_t)blockIdx.y * JOIN_COLS + lane_id(); key[e] < (uint32_t)n && c < min(p, ((int64_t)blockIdx.y + 1) * JOIN_COLS); c += 32)
-                de[(int64_t)key[e] * ldde + c] = narrow<G>(A(CUDART_NAN_F));
-        return;
-    }
+    link(key, part);
     const int lane = lane_id(), warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.y * JOIN_COLS + lane, first = (int64_t)blockIdx.x * JOIN + warp * JOIN_EACH;
     auto write = [&](uint32_t id, A(&x)[N]) {
@@ -475,6 +468,11 @@ __global__ void __launch_bounds__(THREADS) join_kernel(int64_t nnz, int64_t n, i
             for (int i = 0; i < N; ++i)
                 if (c + i * 32 < p) part_out[((int64_t)blockIdx.x * 2 + slot) * p + c + i * 32] = x[i];
         });
+    if (err && *err) {  // (the last block of all) a wait among the radix passes has run out, which should not happen: what the entries name becomes NaN
+        for (int64_t e = 0; e < nnz; ++e)
+            for (int i = 0; i < N; ++i)
+                if (key[e] < (uint32_t)n && c + i * 32 < p) de[(int64_t)key[e] * ldde + c + i * 32] = narrow<G>(A(CUDART_NAN_F));
+    }
 }
 
 template <typename T, typename G, int V>
@@ -508,7 +506,7 @@ spsyrk_status_t add_typed(const GradWs& w, int which, const uint32_t* err, const
         cfg.numAttrs = 1;
         A* const out = level + 1 < JOIN_LEVELS ? static_cast<A*>(w.part[level + 1]) : nullptr;  // (null where one block holds all: nothing leaves it)
         SPSYRK_CUDA_TRY(launch_kernel(cfg, join_kernel<A, G>, nnz, n, p, key, static_cast<const A*>(w.part[level]), out, (A)scale, static_cast<G*>(de), ldde,
-                                      accumulate, piece, err));
+                                      accumulate, piece, blocks == 1 ? err : nullptr));
         piece *= JOIN;
         pieces = blocks;
     }
