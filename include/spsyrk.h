@@ -416,6 +416,7 @@ spsyrk_status_t spsyrk_lookup(int64_t m, int64_t n, int64_t p, int64_t nnz, spsy
  * dY is m x p of `dtype`; dE is n x p of `g_dtype`, which is `dtype` or, for half precision, SPSYRK_F32 (a gradient that is kept
  * in single precision).  accumulate == 0: dE is overwritten, zeros in the rows of ids that do not occur.
  * accumulate != 0: dE += the gradient, one more addition before the rounding; the rows of ids that do not occur are not touched.
+ * dE must not alias dY.
  *
  * Two-step use: d_workspace == NULL: *workspace_bytes receives the scratch size for (m, n, p, nnz, dtype) with and without row pointers
  * and weights; then the call, with a workspace of at least that size, 256-byte aligned, that no other work uses until this has ended.

@@ -1,7 +1,9 @@
 // Y = scale * A E for rows of ids A and a dense table E (an embedding lookup, or sums over bags of ids), and the gradient of the
 // weights, dw_t = scale * <E[id_t], dY[row of t]>.
 //
-// Both move every row of E that they name and do two operations per element: bound by memory, or by latency for few rows.
+// Both move every row of E that they name and do two operations per element: bound by memory where rows are wide, by latency for few rows, and
+// by latency for sums over many narrow rows (10000 sets of up to 140 rows of 64 floats 52 us, their weights' gradient 60: issue slots half used, 26 and
+// 33 % of an SM's warps, L2 at 9 %).
 // A group of 1 to 256 lanes holds a row of Y, 16 bytes a lane, and keeps its sum in registers.
 #include <algorithm>
 
