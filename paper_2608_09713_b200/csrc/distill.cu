@@ -9,7 +9,9 @@
 // way: six CTAs per SM, and one instruction that asks for the whole share to be brought to L2 before the teacher's entries are looked at
 // (422 us without it, 389 with it for 4096 rows of 131072 bfloat16 logits, 2.1 GB; now 373, 88 % of the copy rate).  Kept in shared memory instead
 // of L2 only three shares fit an SM (513 us; with CTAs that stay and copy the next row meanwhile 660, whose rows wait for one another).
-// exp(x) is computed as 2^(s * log2(e) / tau - ...): a multiply-add (two logits per instruction) and an exponential per logit.
+// exp(x) is computed as 2^(s * log2(e) / tau - ...): a multiply-add and an exponential per logit.  (Instructions for two floats at a time, f32x2,
+// are no faster here, and with their operands in register pairs the half-precision gradient that goes by the shift came out with infinities, now and then, in
+// warps whose lanes did not all take as many turns of the loop.)
 // The gradient is first written for all ids as if they were not the teacher's, then the few of the teacher's are overwritten, from
 // logits that were fetched beforehand (so the gradient may overwrite the logits).  An id that occurs more than once is written for one
 // of its entries, with the sum of all in their order: they are found with a hash table in shared memory.  Rows of more than
@@ -107,43 +109,13 @@ __device__ __forceinline__ Running join(Running r, float k) {
     return Running{top, r.sum};
 }
 
-// Two single-precision numbers in one register pair, for the instructions that take two at a time.
-struct Pair {
-    uint64_t v;
-};
-__device__ __forceinline__ Pair pair(float lo, float hi) {
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
-    return p;
-}
-__device__ __forceinline__ float2 halves(Pair p) {
-    float2 f;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
-    return f;
-}
-__device__ __forceinline__ Pair multiply_add(Pair a, Pair b, Pair c) {
-    Pair d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return d;
-}
-__device__ __forceinline__ Pair add(Pair a, Pair b) {
-    Pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
-    return d;
-}
-__device__ __forceinline__ Pair multiply(Pair a, Pair b) {
-    Pair d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d.v) : "l"(a.v), "l"(b.v));
-    return d;
-}
-
 // 16 bytes of logits as pairs, their largest value, and back
 template <typename T> struct Unit;
 template <> struct Unit<float> {
     static constexpr int PAIRS = 2;
     static constexpr uint32_t NOTHING = 0xff800000u;  // -infinity
-    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
-        return i == 0 ? pair(__uint_as_float(u.x), __uint_as_float(u.y)) : pair(__uint_as_float(u.z), __uint_as_float(u.w));
+    __device__ static __forceinline__ float2 get(const uint4& u, int i) {
+        return i == 0 ? float2{__uint_as_float(u.x), __uint_as_float(u.y)} : float2{__uint_as_float(u.z), __uint_as_float(u.w)};
     }
     template <int U>
     __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
@@ -163,8 +135,8 @@ __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 
 template <> struct Unit<__nv_bfloat16> {
     static constexpr int PAIRS = 4;
     static constexpr uint32_t NOTHING = 0xff80ff80u;
-    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
-        return pair(__uint_as_float(word(u, i) << 16), __uint_as_float(word(u, i) & 0xffff0000u));
+    __device__ static __forceinline__ float2 get(const uint4& u, int i) {
+        return float2{__uint_as_float(word(u, i) << 16), __uint_as_float(word(u, i) & 0xffff0000u)};
     }
     template <int U>
     __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
@@ -189,10 +161,9 @@ template <> struct Unit<__nv_bfloat16> {
 template <> struct Unit<__half> {
     static constexpr int PAIRS = 4;
     static constexpr uint32_t NOTHING = 0xfc00fc00u;
-    __device__ static __forceinline__ Pair get(const uint4& u, int i) {
+    __device__ static __forceinline__ float2 get(const uint4& u, int i) {
         const uint32_t w = word(u, i);
-        const float2 f = __half22float2(reinterpret_cast<const __half2&>(w));
-        return pair(f.x, f.y);
+        return __half22float2(reinterpret_cast<const __half2&>(w));
     }
     template <int U>
     __device__ static __forceinline__ float largest(const uint4 (&u)[U]) {
@@ -226,19 +197,18 @@ __device__ __forceinline__ void take_units(Running& r, const uint4 (&u)[U], floa
     }
     const float b = base_of(r.most), at = __fmul_rn(b, k);
     if (fabsf(at) < NEAR) {
-        const Pair kk = pair(k, k), off = pair(-at, -at);
-        Pair sum[2] = {pair(r.sum, 0.f), pair(0.f, 0.f)};
+        float2 sum[2] = {{r.sum, 0.f}, {0.f, 0.f}};
 #pragma unroll
         for (int i = 0; i < U * PAIRS; ++i) {
-            const float2 x = halves(multiply_add(Unit<T>::get(u[i / PAIRS], i % PAIRS), kk, off));
-            sum[i & 1] = add(sum[i & 1], pair(power_of_two(x.x), power_of_two(x.y)));
+            const float2 x = Unit<T>::get(u[i / PAIRS], i % PAIRS);
+            sum[i & 1].x += power_of_two(fmaf(x.x, k, -at));
+            sum[i & 1].y += power_of_two(fmaf(x.y, k, -at));
         }
-        const float2 s = halves(add(sum[0], sum[1]));
-        r.sum = s.x + s.y;
+        r.sum = (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
     } else {
 #pragma unroll
         for (int i = 0; i < U * PAIRS; ++i) {
-            const float2 x = halves(Unit<T>::get(u[i / PAIRS], i % PAIRS));
+            const float2 x = Unit<T>::get(u[i / PAIRS], i % PAIRS);
             r.sum += power_of_two((x.x - b) * k) + power_of_two((x.y - b) * k);
         }
     }
@@ -289,15 +259,14 @@ enum Form { FOLDED, BY_SHIFT, BY_BASE };
 template <typename T, int THREADS, Form FORM>
 __device__ __forceinline__ void write_units(const uint4* at, uint4* to, int left, float k, float shift, float a) {
     constexpr int U = 4, PAIRS = Unit<T>::PAIRS;
-    const Pair kk = pair(k, k), off = pair(-shift, -shift), aa = pair(a, a);
     auto of = [&](const uint4& x) {
         float2 y[PAIRS];
 #pragma unroll
         for (int q = 0; q < PAIRS; ++q) {
-            const Pair s = Unit<T>::get(x, q);
-            const float2 p = halves(FORM == BY_BASE ? multiply(add(s, off), kk) : multiply_add(s, kk, off));
-            y[q] = float2{power_of_two(p.x), power_of_two(p.y)};
-            if (FORM != FOLDED) y[q] = halves(multiply(pair(y[q].x, y[q].y), aa));
+            const float2 s = Unit<T>::get(x, q);
+            y[q] = FORM == BY_BASE ? float2{power_of_two((s.x - shift) * k), power_of_two((s.y - shift) * k)}
+                                   : float2{power_of_two(fmaf(s.x, k, -shift)), power_of_two(fmaf(s.y, k, -shift))};
+            if (FORM != FOLDED) y[q] = float2{a * y[q].x, a * y[q].y};
         }
         return Unit<T>::put(y);
     };
@@ -527,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, WARPS_PER_SM * 32 / THREADS) distill_
     bool all = true;  // a wait that runs out, which should not happen, is seen in the results: NaN
     if (size > 1) {
         all = barrier_wait(&s_arrived, 0);  // from here on logits may be overwritten: all have fetched the teacher's
-        if (sums) {
+            if (sums) {
             const float2 part = s_cta[lane_id() & (size - 1)];
             r = Running{part.x, all ? part.y : CUDART_NAN_F};
             r = size == 2 ? join<2>(r, c.k) : size == 4 ? join<4>(r, c.k) : join<8>(r, c.k);

@@ -211,3 +211,26 @@ def test_a_norm_that_leaves_the_teacher_nothing(B, norm):
     loss, lse, grad = B.spsyrk_distill(logits, ids, z, teacher_lse=torch.full((6,), norm, device="cuda"), grad=True)
     assert (loss[[0, 1, 5]] == 0).all() and (grad[[0, 1, 5]] == 0).all()
     assert loss[2:5].isnan().all() and grad[2:5].isnan().all()
+
+
+@pytest.mark.parametrize("m,n,k", [(950, 3157, 256), (16, 7000, 256), (300, 7000, 120), (64, 333, 30)])
+@pytest.mark.parametrize("base", [3.0, -500.0, -2000.0, 2700.0, -7000.0])
+@pytest.mark.parametrize("dtype", LOGITS)
+def test_the_same_call_gives_the_same_bits(B, dtype, base, m, n, k):
+    """Rows whose units and teacher's entries do not fill the last turn of a warp, ids that occur twice: every repetition, right and alike."""
+    gen = _gen(n + k)
+    for spread in (0.0, 1.0):
+        logits = (base + spread * torch.randn((m, n), generator=gen, device="cuda")).to(dtype)
+        ids = torch.randint(0, n // 2, (m, k), generator=gen, device="cuda", dtype=torch.int32)
+        z = (base + torch.randn((m, k), generator=gen, device="cuda")).to(dtype)
+        first = None
+        for _ in range(40):
+            loss, lse, grad = B.spsyrk_distill(logits, ids, z, grad=True)
+            out = (loss, lse, grad, B.spsyrk_distill_grad(logits, lse, ids, z))
+            first = first or [t.clone() for t in out]
+            assert all(torch.equal(a, b) for a, b in zip(out, first))
+        # (double precision over all rows at once; a row's q is at most one: 2^-9 of it and of p, and the steps of the type's smallest numbers)
+        logp = torch.log_softmax(z.double(), 1)
+        expected = torch.softmax(logits.double(), 1).scatter_add_(1, ids.long(), -logp.exp())
+        size = torch.softmax(logits.double(), 1).scatter_add_(1, ids.long(), logp.exp())
+        assert ((first[2].double() - expected).abs() <= size * (torch.finfo(dtype).eps / 2 + 2.0 ** -12) + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps).all()
